@@ -1,5 +1,6 @@
 """Builds libenec.so (the CUDA library) in-tree with nvcc for sm_100a. Cross-compiles without a GPU."""
 import os
+import re
 import subprocess
 import sys
 
@@ -21,6 +22,18 @@ def _deps():
     return deps
 
 
+def _deps_of(path, seen=None):
+    """The file and every header of this project that it includes, directly or not."""
+    seen = set() if seen is None else seen
+    if path not in seen:
+        seen.add(path)
+        for name in re.findall(r'^\s*#include "([^"]+)"', open(path).read(), flags=re.M):
+            for folder in (CSRC, INCLUDE):
+                if os.path.exists(os.path.join(folder, name)):
+                    _deps_of(os.path.join(folder, name), seen)
+    return seen
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if (not force and os.path.exists(LIB)
             and all(os.path.getmtime(LIB) >= os.path.getmtime(d) for d in _deps())):
@@ -34,7 +47,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         obj = os.path.join(objdir, os.path.basename(src)[:-3] + ".o")
         objs.append(obj)
         if (not force and os.path.exists(obj)
-                and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in _deps())):
+                and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in _deps_of(src))):
             continue
         cmd = [nvcc, *NVCC_FLAGS, "-c", src, "-o", obj]
         if verbose:
