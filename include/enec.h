@@ -198,6 +198,50 @@ enec_status enec_compress_batched(const enec_batch_item* h_items, int n_items, e
 enec_status enec_compress_noalloc(const void* d_in, enec_dtype dt, size_t count, void* d_out, size_t out_capacity,
                                   size_t* d_out_size, int* d_status, enec_stream_t stream);
 
+/*
+ * ---- Microscaled 4-bit streams: lossy, 4.25 bits a value, and products that read them --------------------------------------------
+ *
+ * The MXFP4 form of the OCP microscaling formats: values in E2M1 (sign, two exponent bits, one mantissa bit: 0, .5, 1, 1.5, 2, 3, 4,
+ * 6) with one E8M0 scale, a power of two, for every 32 neighbouring values of a row. A block with a = max |x| has the scale 2^s,
+ * s = clamp(floor(log2 a) - 2, -127, 127); every value x 2^-s is rounded once to the nearest E2M1 value, ties to the even code,
+ * values above 6 to 6; a block that holds a NaN or an infinity is a block of NaN. The last block of a row may be shorter.
+ *
+ * A stream holds `batch` matrices of rows x cols values (all below 2^31; ENEC_ERR_TOO_LARGE beyond 2^29 records). Its layout,
+ * little-endian:
+ *   bytes 0..31  u32 magic "ENM4", u32 version 1, u32 batch, u32 rows, u32 cols, u32 0, u64 length of the stream; 32..127 zero
+ *   then for every matrix, for every 128 rows, for every 256 columns (fastest) a record of 17408 bytes: row r of the record
+ *   at 128 r, and in it columns 32c .. 32c + 31 in the 16 bytes at 16 (c xor (r mod 8)), the lower four bits of a byte first; from byte
+ *   16384 on the scale bytes (127 + s; 255: NaN, all elements zero), that of row r and columns 32c .. at 512 (c / 4) + 16 (r mod
+ *   32) + 4 (r / 32) + c mod 4. Rows and columns of a record behind the matrix are zero bytes.
+ * The stream has no checksum: a call checks the header against its own arguments (ENEC_ERR_BAD_STREAM in *d_status, and the output
+ * is left as it was); other damage gives other values, never an access out of range.
+ *
+ * The conventions are those of the codec above, with two additions. Matrices in ordinary types are row-major with `ld` values from the
+ * beginning of a row to that of the next (ld >= cols; matrix b of a batch begins at b * rows * ld); what lies between rows is neither
+ * read into results nor written. And all these calls can be captured into a CUDA graph and may run on several streams at once: they
+ * keep no state from call to call and allocate nothing.
+ */
+
+/* Length of a stream; 0 where the shape is too large. Pure host function. */
+size_t enec_microscaled_size(size_t batch, size_t rows, size_t cols);
+
+/* Quantises [batch, rows, cols] values of type dt into the stream at d_out (out_capacity at least enec_microscaled_size). */
+enec_status enec_quantize_microscaled(const void* d_in, enec_dtype dt, size_t batch, size_t rows, size_t cols, size_t ld, void* d_out,
+                                      size_t out_capacity, int* d_status, enec_stream_t stream);
+
+/* The values of a stream in type dt: exact in bf16 and fp32 (magnitudes beyond the type's range become infinities), rounded once
+ * in fp16. */
+enec_status enec_dequantize_microscaled(const void* d_in, size_t in_size, enec_dtype dt, size_t batch, size_t rows, size_t cols,
+                                        void* d_out, size_t ld, int* d_status, enec_stream_t stream);
+
+/*
+ * y = x W^T: x [tokens, cols] and y [tokens, rows] of type dt (bf16 or fp16), W a stream of one matrix of rows x cols. Sums are in fp32,
+ * y is rounded once; neither x nor W is rounded on the way. From one token (bound by the weights' bytes) to thousands (tensor
+ * cores). tokens == 0 or rows == 0 is valid and does nothing; cols == 0 gives zeros. x and y must not overlap.
+ */
+enec_status enec_matmul_microscaled(const void* d_x, enec_dtype dt, size_t tokens, size_t ld_x, const void* d_w, size_t w_size,
+                                    size_t rows, size_t cols, void* d_y, size_t ld_y, int* d_status, enec_stream_t stream);
+
 /* Number of kernels the library has launched in this process (all entry points, all streams). */
 uint64_t enec_launch_count(void);
 

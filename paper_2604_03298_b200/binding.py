@@ -65,6 +65,17 @@ def lib():
         L.enec_decompress_batched.restype = C.c_int
         L.enec_compress_batched.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
         L.enec_compress_batched.restype = C.c_int
+        L.enec_microscaled_size.argtypes = [C.c_size_t] * 3
+        L.enec_microscaled_size.restype = C.c_size_t
+        L.enec_quantize_microscaled.argtypes = [C.c_void_p, C.c_int, C.c_size_t, C.c_size_t, C.c_size_t, C.c_size_t, C.c_void_p, C.c_size_t,
+                                                C.c_void_p, C.c_void_p]
+        L.enec_quantize_microscaled.restype = C.c_int
+        L.enec_dequantize_microscaled.argtypes = [C.c_void_p, C.c_size_t, C.c_int, C.c_size_t, C.c_size_t, C.c_size_t, C.c_void_p, C.c_size_t,
+                                                  C.c_void_p, C.c_void_p]
+        L.enec_dequantize_microscaled.restype = C.c_int
+        L.enec_matmul_microscaled.argtypes = [C.c_void_p, C.c_int, C.c_size_t, C.c_size_t, C.c_void_p, C.c_size_t, C.c_size_t, C.c_size_t,
+                                              C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        L.enec_matmul_microscaled.restype = C.c_int
         L.enec_launch_count.argtypes = []
         L.enec_launch_count.restype = C.c_uint64
         L.enec_allocation_count.argtypes = []
@@ -163,6 +174,26 @@ def enec_compress_batched(items, dt, d_out_sizes=None, d_status=None) -> int:
                                        _stream())
 
 
+def enec_microscaled_size(batch: int, rows: int, cols: int) -> int:
+    """Bytes of a microscaled 4-bit stream of `batch` matrices of rows x cols values."""
+    return lib().enec_microscaled_size(batch, rows, cols)
+
+
+def enec_quantize_microscaled(d_in, dt, batch, rows, cols, ld, d_out, out_capacity, d_status=None) -> int:
+    """[batch, rows, cols] values, rows `ld` values apart, into the microscaled stream d_out."""
+    return lib().enec_quantize_microscaled(_ptr(d_in), dt, batch, rows, cols, ld, _ptr(d_out), out_capacity, _ptr(d_status), _stream())
+
+
+def enec_dequantize_microscaled(d_in, in_size, dt, batch, rows, cols, d_out, ld, d_status=None) -> int:
+    """The values of a microscaled stream in type dt, rows `ld` values apart."""
+    return lib().enec_dequantize_microscaled(_ptr(d_in), in_size, dt, batch, rows, cols, _ptr(d_out), ld, _ptr(d_status), _stream())
+
+
+def enec_matmul_microscaled(d_x, dt, tokens, ld_x, d_w, w_size, rows, cols, d_y, ld_y, d_status=None) -> int:
+    """d_y [tokens, rows] = d_x [tokens, cols] times the transpose of the microscaled stream d_w (one matrix of rows x cols)."""
+    return lib().enec_matmul_microscaled(_ptr(d_x), dt, tokens, ld_x, _ptr(d_w), w_size, rows, cols, _ptr(d_y), ld_y, _ptr(d_status), _stream())
+
+
 def enec_launch_count() -> int:
     return lib().enec_launch_count()
 
@@ -247,4 +278,40 @@ def decompress_tensor(stream: torch.Tensor, dtype: torch.dtype, shape) -> torch.
     a, stream_handle = _answer()
     st = lib().enec_decompress(stream.data_ptr(), stream.numel(), dt, out.numel(), out.data_ptr(), a.status_at, stream_handle)
     _finish(a, st, "enec_decompress")
+    return out
+
+
+def quantize_tensor(t: torch.Tensor) -> torch.Tensor:
+    """The microscaled 4-bit stream (uint8) of a CUDA bf16/fp16/fp32 tensor of two or three dimensions ([batch,] rows, cols); the
+    last dimension has to be dense, rows may lie apart. Lossy: 32 neighbouring values of a row share a power of two."""
+    dt = _DT[t.dtype]
+    if t.dim() not in (2, 3):
+        raise ValueError("a microscaled stream holds matrices: two or three dimensions")
+    t = t if t.dim() == 3 else t.unsqueeze(0)
+    batch, rows, cols = t.shape
+    ld = t.stride(1)
+    if (cols > 1 and t.stride(2) != 1) or ld < cols or (batch > 1 and t.stride(0) != rows * ld) or t.data_ptr() % 16:
+        t = t.contiguous()
+        if t.data_ptr() % 16:
+            t = t.clone()
+        ld = cols
+    size = enec_microscaled_size(batch, rows, cols)
+    if size == 0:
+        raise EnecError(-8, "enec_microscaled_size")
+    out = torch.empty(size, dtype=torch.uint8, device=t.device)
+    st = enec_quantize_microscaled(t, dt, batch, rows, cols, ld, out, size)
+    if st != 0:
+        raise EnecError(st, "enec_quantize_microscaled")
+    return out
+
+
+def dequantize_tensor(stream: torch.Tensor, dtype: torch.dtype, shape) -> torch.Tensor:
+    """The values of a stream of quantize_tensor in `dtype`; waits for the current stream once to learn whether the header fits."""
+    shape = tuple(shape)
+    batch, rows, cols = shape if len(shape) == 3 else (1, *shape)
+    out = torch.empty(shape, dtype=dtype, device=stream.device)
+    a, stream_handle = _answer()
+    st = lib().enec_dequantize_microscaled(stream.data_ptr(), stream.numel(), _DT[dtype], batch, rows, cols, out.data_ptr(), cols, a.status_at,
+                                           stream_handle)
+    _finish(a, st, "enec_dequantize_microscaled")
     return out

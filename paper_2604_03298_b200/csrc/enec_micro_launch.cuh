@@ -1,0 +1,27 @@
+// The product's forms, as its entry point chooses among them.
+#pragma once
+
+#include "enec_micro.cuh"
+
+namespace enec {
+
+struct MicroProduct {
+    int dt;
+    const uint8_t* x;
+    uint64_t ld_x;
+    uint32_t tokens;
+    const uint8_t* w;
+    MicroShape s;      // of w
+    uint8_t* y;
+    uint64_t ld_y;
+    int* status;
+};
+
+constexpr uint32_t kFewMostShared = 227 * 1024;
+
+// The most tokens one launch for few tokens takes with rows of `cols` values (32, or fewer where they would not fit; 0 where not one does).
+uint32_t micro_few_most_tokens(uint32_t cols);
+// Tokens first .. first + tokens - 1 of the product.
+enec_status micro_few(const MicroProduct& p, uint32_t first, uint32_t tokens, const MicroDevice& dev, cudaStream_t stream);
+
+}  // namespace enec

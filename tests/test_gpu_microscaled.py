@@ -1,0 +1,242 @@
+"""Microscaled 4-bit streams on the GPU: bytes, values and products against plain numpy in 64 bits (microscaled_reference)."""
+import numpy as np
+import pytest
+import torch
+
+import microscaled_reference as ref
+from gpu_util import status_tensor
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {0: torch.bfloat16, 1: torch.float16, 2: torch.float32}
+HALF_STEP = {dt: torch.finfo(t).eps / 2 for dt, t in DTYPES.items()}   # of a rounding, relative to the value
+
+
+def enec():
+    import paper_2604_03298_b200
+    return paper_2604_03298_b200
+
+
+def drawn(shape, dt, seed, kind="normal"):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g)
+    if kind == "wide":       # exponents all over the type's range, zeros, the largest and the smallest values
+        limit = {0: 120, 1: 13, 2: 120}[dt]
+        x = x * torch.exp2(torch.randint(-limit, limit, (*shape[:-1], 1), generator=g).float())
+        x = torch.where(torch.rand(shape, generator=g) < 0.1, torch.zeros(()), x)
+    if kind == "grid":       # borders and ties
+        x = torch.randint(-32, 33, shape, generator=g).float() / 4
+    return x.to(DTYPES[dt])
+
+
+def strided(x, gap, fill):
+    """x on the GPU in rows `gap` values further apart, the gaps filled with `fill`."""
+    wide = torch.full((*x.shape[:-1], x.shape[-1] + gap), fill, dtype=x.dtype)
+    wide[..., :x.shape[-1]] = x
+    return wide.cuda()
+
+
+SHAPES = [(1, 1, 1), (1, 1, 32), (1, 3, 33), (1, 128, 256), (1, 129, 257), (2, 37, 100), (3, 127, 511), (1, 300, 2047), (2, 5, 8)]
+
+
+@pytest.mark.parametrize("dt", [0, 1, 2])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("kind, gap", [("normal", 0), ("wide", 1), ("grid", 3), ("normal", 8)])
+def test_stream_is_the_definitions_byte_for_byte(dt, shape, kind, gap):
+    E = enec()
+    x = drawn(shape, dt, 100 * dt + 7 * shape[1] + shape[2], kind)
+    size = E.enec_microscaled_size(*shape)
+    buf = torch.full((size + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+    status = status_tensor()
+    assert E.enec_quantize_microscaled(strided(x, gap, float("nan")), dt, *shape, shape[2] + gap, buf, size, status) == 0
+    got = buf.cpu().numpy()
+    assert int(status.item()) == 0
+    assert np.array_equal(got[:size], ref.stream(x.double().numpy()))
+    assert (got[size:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("dt", [0, 1, 2])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("gap", [0, 1, 3, 8])
+def test_values_of_a_stream(dt, shape, gap):
+    """Exact in bf16 and fp32; in fp16 the nearest value, which torch's conversion of the exact one gives. Gaps stay as they were."""
+    E = enec()
+    x = drawn(shape, 2, 11 + shape[2], "normal") * 0.3
+    stream = torch.from_numpy(ref.stream(x.double().numpy())).cuda()
+    out = torch.full((*shape[:-1], shape[2] + gap), 7.0, dtype=DTYPES[dt], device="cuda")
+    status = status_tensor()
+    assert E.enec_dequantize_microscaled(stream, stream.numel(), dt, *shape, out, shape[2] + gap, status) == 0
+    got = out.cpu()
+    assert int(status.item()) == 0
+    assert torch.equal(got[..., :shape[2]], torch.from_numpy(ref.values(x.double().numpy())).to(DTYPES[dt]))
+    assert (got[..., shape[2]:] == 7).all()
+
+
+@pytest.mark.parametrize("dt", [0, 1, 2])
+def test_extreme_blocks(dt):
+    """Infinities and NaN make their block NaN and no other; zeros keep their sign; the smallest and largest finite values."""
+    E = enec()
+    info = torch.finfo(DTYPES[dt])
+    x = torch.ones(10, 96)
+    x[0, 5], x[1, 40], x[2, 95] = float("inf"), float("-inf"), float("nan")
+    x[3] = 0.0
+    x[4] = -0.0
+    x[5], x[6] = info.max, -info.max
+    x[7] = info.tiny
+    x[8] = info.smallest_normal * info.eps          # the smallest subnormal number
+    x[9, ::2] = info.max
+    x = x.to(DTYPES[dt])
+    stream = E.quantize_tensor(x.cuda())
+    assert np.array_equal(stream.cpu().numpy(), ref.stream(x.double().numpy()[None]))
+    back = E.dequantize_tensor(stream, DTYPES[dt], x.shape).cpu()
+    want = torch.from_numpy(ref.values(x.double().numpy())).to(DTYPES[dt])
+    assert torch.equal(torch.isnan(back), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(back), torch.nan_to_num(want))
+    assert torch.isnan(back[0, :32]).all() and not torch.isnan(back[0, 32:]).any()
+
+
+def test_empty_shapes_and_wrong_headers():
+    E = enec()
+    status = status_tensor()
+    for shape in ((0, 4, 4), (2, 0, 7), (2, 3, 0)):
+        size = E.enec_microscaled_size(*shape)
+        buf = torch.zeros(size, dtype=torch.uint8, device="cuda")
+        assert E.enec_quantize_microscaled(None, 0, *shape, max(shape[2], 1), buf, size, status) == 0
+        assert np.array_equal(buf.cpu().numpy(), ref.stream(np.zeros(shape)))
+        assert E.enec_dequantize_microscaled(buf, size, 0, *shape, None, max(shape[2], 1), status) == 0
+        assert int(status.item()) == 0
+    x = drawn((5, 300), 0, 3).cuda()
+    stream = E.quantize_tensor(x)
+    for at, shape in ((0, (5, 300)), (4, (5, 300)), (8, (5, 300)), (24, (5, 300)), (None, (4, 300)), (None, (5, 299))):
+        bad = stream.clone()
+        if at is not None:
+            bad[at] += 1
+        out = torch.full(shape, 3.0, dtype=torch.bfloat16, device="cuda")
+        y = torch.full((2, shape[0]), 3.0, dtype=torch.bfloat16, device="cuda")
+        status.zero_()
+        assert E.enec_dequantize_microscaled(bad, bad.numel(), 0, 1, *shape, out, shape[1], status) == 0
+        assert int(status.item()) == -4 and (out == 3).all()
+        status.zero_()
+        assert E.enec_matmul_microscaled(x, 0, 2, 300, bad, bad.numel(), *shape, y, shape[0], status) == 0
+        assert int(status.item()) == -4 and (y == 3).all()
+        with pytest.raises(E.EnecError):
+            E.dequantize_tensor(bad, torch.bfloat16, shape)
+
+
+def product_bound(x, w, dt):
+    """How far a product may be off: its own rounding, and fp32 sums. Every term is exact or within 2^-24 of its row's largest
+    (activations scaled to fp16: 2^-39 of the row's largest, far less); n terms added in any order with at most n roundings of
+    2^-24 relative to the sum of magnitudes."""
+    magnitudes = np.abs(x) @ np.abs(w).T
+    top = np.abs(x).max(-1, keepdims=True) * np.abs(w).sum(-1)[None, :]
+    exact = x @ w.T
+    return exact, HALF_STEP[dt] * np.abs(exact) + (x.shape[1] + 16) * 2.0 ** -24 * magnitudes + 2.0 ** -38 * top
+
+
+def check_product(tokens, rows, cols, dt, gap_x=0, gap_y=0, scale=1.0, seed=0, call="enec_matmul_microscaled"):
+    E = enec()
+    g = torch.Generator().manual_seed(seed + tokens * 7 + rows * 3 + cols)
+    x = (torch.randn(tokens, cols, generator=g) * scale).to(DTYPES[dt])
+    w = torch.randn(rows, cols, generator=g) * torch.exp2(torch.randint(-6, 3, (rows, 1), generator=g).float())
+    stream = torch.from_numpy(ref.stream(w.double().numpy()[None])).cuda()
+    values = ref.values(w.double().numpy())
+    y = torch.full((tokens, rows + gap_y), 5.0, dtype=DTYPES[dt], device="cuda")
+    status = status_tensor()
+    assert E.enec_matmul_microscaled(strided(x, gap_x, float("nan")), dt, tokens, cols + gap_x, stream, stream.numel(), rows, cols, y, rows + gap_y,
+                                     status) == 0
+    got = y.cpu().double().numpy()
+    assert int(status.item()) == 0
+    exact, bound = product_bound(x.double().numpy(), values, dt)
+    tiny = torch.finfo(DTYPES[dt]).smallest_normal * torch.finfo(DTYPES[dt]).eps
+    off = np.abs(got[:, :rows] - exact)
+    assert (off <= bound + tiny / 2).all(), (off / (bound + tiny)).max()
+    assert (got[:, rows:] == 5).all()
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("tokens", [1, 2, 7, 8, 9, 16, 17, 32, 33, 100])
+@pytest.mark.parametrize("rows, cols", [(1, 1), (16, 128), (129, 300), (100, 1408), (515, 2055)])
+def test_product(dt, tokens, rows, cols):
+    check_product(tokens, rows, cols, dt)
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("tokens", [1, 5, 40, 130])
+@pytest.mark.parametrize("gap_x, gap_y", [(1, 0), (8, 3), (0, 1), (3, 8)])
+def test_product_with_rows_apart(dt, tokens, gap_x, gap_y):
+    check_product(tokens, 200, 333, dt, gap_x, gap_y)
+    check_product(tokens, 256, 512, dt, gap_x, gap_y)
+
+
+@pytest.mark.parametrize("tokens", [1, 8, 32, 200])
+@pytest.mark.parametrize("scale", [1e-30, 1e-6, 1e5, 1e30])
+def test_product_of_small_and_large_activations(tokens, scale):
+    check_product(tokens, 130, 700, 0, scale=scale)
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("tokens, rows, cols", [(8, 48, 14336), (32, 40, 14336), (3, 20, 60000), (1, 4096, 4096), (65, 20, 20000)])
+def test_product_of_long_rows(dt, tokens, rows, cols):
+    check_product(tokens, rows, cols, dt)
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("tokens", [2, 140])
+def test_infinities_and_nan_stay_in_their_token_and_their_row(dt, tokens):
+    """An infinity in a token's row: sums of that token are infinite or NaN as the weights say, others as without it. A weight block
+    of NaN: its row for every token, others not."""
+    E = enec()
+    x = drawn((tokens, 320), dt, 5)
+    w = drawn((70, 320), 2, 6)
+    clean = E.quantize_tensor(w.cuda())
+    y = torch.empty(tokens, 70, dtype=DTYPES[dt], device="cuda")
+    base = torch.empty_like(y)
+    assert E.enec_matmul_microscaled(x.cuda(), dt, tokens, 320, clean, clean.numel(), 70, 320, base, 70) == 0
+    bad = x.clone()
+    bad[1, 100] = float("inf")
+    assert E.enec_matmul_microscaled(bad.cuda(), dt, tokens, 320, clean, clean.numel(), 70, 320, y, 70) == 0
+    q = torch.from_numpy(ref.values(w.double().numpy()))[:, 100]
+    want = torch.where(q == 0, torch.full_like(q, float("nan")), torch.sign(q) * float("inf"))
+    got = y.cpu().double()
+    assert torch.equal(torch.nan_to_num(got[1], nan=1.0), torch.nan_to_num(want, nan=1.0))
+    assert torch.equal(y[0], base[0]) and torch.equal(y[2:], base[2:])
+    w[3, 7] = float("nan")
+    dirty = E.quantize_tensor(w.cuda())
+    assert E.enec_matmul_microscaled(x.cuda(), dt, tokens, 320, dirty, dirty.numel(), 70, 320, y, 70) == 0
+    assert torch.isnan(y[:, 3]).all()
+    keep = [i for i in range(70) if i != 3]
+    assert torch.equal(y[:, keep], base[:, keep])
+
+
+@pytest.mark.parametrize("tokens", [1, 16, 200])
+def test_product_of_no_columns_is_zero(tokens):
+    E = enec()
+    stream = torch.from_numpy(ref.stream(np.zeros((1, 9, 0)))).cuda()
+    y = torch.full((tokens, 12), 5.0, dtype=torch.float16, device="cuda")
+    assert E.enec_matmul_microscaled(None, 1, tokens, 0, stream, stream.numel(), 9, 0, y, 12) == 0
+    assert (y[:, :9] == 0).all() and (y[:, 9:] == 5).all()
+
+
+@pytest.mark.parametrize("tokens", [1, 8, 50, 300])
+def test_repeated_captured_and_concurrent_calls_agree_bit_for_bit(tokens):
+    E = enec()
+    x, w = drawn((tokens, 1000), 0, 1).cuda(), drawn((300, 1000), 2, 2)
+    stream = E.quantize_tensor(w.cuda())
+    ys = [torch.zeros(tokens, 300, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+
+    def call(y):
+        assert E.enec_matmul_microscaled(x, 0, tokens, 1000, stream, stream.numel(), 300, 1000, y, 300) == 0
+    call(ys[0])
+    torch.cuda.synchronize()
+    side = [torch.cuda.Stream() for _ in range(2)]
+    for s, y in zip(side, ys[1:3]):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            call(y)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call(ys[3])
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(ys[0], y) for y in ys[1:])
