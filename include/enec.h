@@ -242,6 +242,33 @@ enec_status enec_dequantize_microscaled(const void* d_in, size_t in_size, enec_d
 enec_status enec_matmul_microscaled(const void* d_x, enec_dtype dt, size_t tokens, size_t ld_x, const void* d_w, size_t w_size,
                                     size_t rows, size_t cols, void* d_y, size_t ld_y, int* d_status, enec_stream_t stream);
 
+/*
+ * The same product with both operands as streams: X a stream of one matrix of tokens x cols (enec_quantize_microscaled of the
+ * activations), y of type dt. The products of a prompt at the tensor cores' 4-bit rate; what rounding the activations to 4 bits costs
+ * is the caller's decision.
+ */
+enec_status enec_matmul_microscaled_both(const void* d_x, size_t x_size, size_t tokens, const void* d_w, size_t w_size, size_t rows,
+                                         size_t cols, enec_dtype dt, void* d_y, size_t ld_y, int* d_status, enec_stream_t stream);
+
+/*
+ * A mixture-of-experts layer for few tokens, in two launches. x, y [tokens, hidden] and the router [experts, hidden] (dense) of type dt
+ * (bf16 or fp16); gate and up streams of `experts` matrices inter x hidden, down one of `experts` matrices hidden x inter.
+ *   l = x R^T, p = softmax(l); a token's experts are the top_k with the largest l (ties: the lower number; a NaN counts as the
+ *   smallest); their weights are p, with `renormalize` divided by the chosen ones' sum;
+ *   y = sum over the chosen experts of weight * (silu(x G^T) * (x U^T)) D^T, silu(a) = a / (1 + exp(-a)).
+ * Sums are in fp32; the hidden values are rounded to fp16's 11 bits (scaled: no overflow) on their way into the last product, y once.
+ * tokens <= 64, experts <= 512, top_k <= min(16, experts), tokens * experts <= 24576, else ENEC_ERR_TOO_LARGE or, for top_k beyond
+ * experts and for sizes of zero, ENEC_ERR_INVALID_ARG; ENEC_ERR_TOO_LARGE too where not one token's row of hidden or inter values fits
+ * into an SM's shared memory (about 60000 values). tokens == 0 is valid and does nothing.
+ * d_workspace: enec_moe_microscaled_workspace bytes of device memory, 16-byte aligned, of any content; the call uses it from its
+ * beginning to its end, so calls that may overlap on the GPU need one each.
+ */
+size_t enec_moe_microscaled_workspace(size_t tokens, size_t hidden, size_t inter, size_t experts, size_t top_k);
+enec_status enec_moe_microscaled(const void* d_x, enec_dtype dt, size_t tokens, size_t hidden, size_t ld_x, const void* d_router, size_t experts,
+                                 size_t top_k, int renormalize, const void* d_gate, size_t gate_size, const void* d_up, size_t up_size,
+                                 const void* d_down, size_t down_size, size_t inter, void* d_y, size_t ld_y, void* d_workspace,
+                                 size_t workspace_bytes, int* d_status, enec_stream_t stream);
+
 /* Number of kernels the library has launched in this process (all entry points, all streams). */
 uint64_t enec_launch_count(void);
 

@@ -76,6 +76,15 @@ def lib():
         L.enec_matmul_microscaled.argtypes = [C.c_void_p, C.c_int, C.c_size_t, C.c_size_t, C.c_void_p, C.c_size_t, C.c_size_t, C.c_size_t,
                                               C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         L.enec_matmul_microscaled.restype = C.c_int
+        L.enec_matmul_microscaled_both.argtypes = [C.c_void_p, C.c_size_t, C.c_size_t, C.c_void_p, C.c_size_t, C.c_size_t, C.c_size_t, C.c_int,
+                                                   C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        L.enec_matmul_microscaled_both.restype = C.c_int
+        L.enec_moe_microscaled_workspace.argtypes = [C.c_size_t] * 5
+        L.enec_moe_microscaled_workspace.restype = C.c_size_t
+        L.enec_moe_microscaled.argtypes = [C.c_void_p, C.c_int, C.c_size_t, C.c_size_t, C.c_size_t, C.c_void_p, C.c_size_t, C.c_size_t, C.c_int,
+                                           C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_size_t, C.c_void_p,
+                                           C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        L.enec_moe_microscaled.restype = C.c_int
         L.enec_launch_count.argtypes = []
         L.enec_launch_count.restype = C.c_uint64
         L.enec_allocation_count.argtypes = []
@@ -192,6 +201,24 @@ def enec_dequantize_microscaled(d_in, in_size, dt, batch, rows, cols, d_out, ld,
 def enec_matmul_microscaled(d_x, dt, tokens, ld_x, d_w, w_size, rows, cols, d_y, ld_y, d_status=None) -> int:
     """d_y [tokens, rows] = d_x [tokens, cols] times the transpose of the microscaled stream d_w (one matrix of rows x cols)."""
     return lib().enec_matmul_microscaled(_ptr(d_x), dt, tokens, ld_x, _ptr(d_w), w_size, rows, cols, _ptr(d_y), ld_y, _ptr(d_status), _stream())
+
+
+def enec_matmul_microscaled_both(d_x, x_size, tokens, d_w, w_size, rows, cols, dt, d_y, ld_y, d_status=None) -> int:
+    """The product of two microscaled streams, d_x (tokens x cols) and d_w (rows x cols), in type dt."""
+    return lib().enec_matmul_microscaled_both(_ptr(d_x), x_size, tokens, _ptr(d_w), w_size, rows, cols, dt, _ptr(d_y), ld_y, _ptr(d_status),
+                                              _stream())
+
+
+def enec_moe_microscaled_workspace(tokens: int, hidden: int, inter: int, experts: int, top_k: int) -> int:
+    return lib().enec_moe_microscaled_workspace(tokens, hidden, inter, experts, top_k)
+
+
+def enec_moe_microscaled(d_x, dt, tokens, hidden, ld_x, d_router, experts, top_k, renormalize, d_gate, gate_size, d_up, up_size, d_down, down_size,
+                         inter, d_y, ld_y, d_workspace, workspace_bytes, d_status=None) -> int:
+    """A mixture-of-experts layer for few tokens; gate, up and down are microscaled streams of `experts` matrices."""
+    return lib().enec_moe_microscaled(_ptr(d_x), dt, tokens, hidden, ld_x, _ptr(d_router), experts, top_k, int(bool(renormalize)), _ptr(d_gate),
+                                      gate_size, _ptr(d_up), up_size, _ptr(d_down), down_size, inter, _ptr(d_y), ld_y, _ptr(d_workspace),
+                                      workspace_bytes, _ptr(d_status), _stream())
 
 
 def enec_launch_count() -> int:

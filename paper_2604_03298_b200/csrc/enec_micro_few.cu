@@ -118,7 +118,7 @@ enec_status launch(FewJob job, const MicroDevice& dev, cudaStream_t stream) {
     if (bytes > kFewMostShared) return ENEC_ERR_TOO_LARGE;
     static std::atomic<uint64_t> allowed{0};
     if (!allow_shared(allowed, dev, enec_micro_few_kernel<DT, NT>, kFewMostShared)) return ENEC_ERR_CUDA;
-    const uint32_t resident = uint32_t(dev.sms) * (bytes <= kFewMostShared / 2 ? 2 : 1) / cluster;
+    const uint32_t resident = uint32_t(dev.sms) * (bytes <= kFewHalfShared ? 2 : 1) / cluster;
     const uint32_t teams = job.strips < resident ? job.strips : resident;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(teams * cluster);

@@ -11,8 +11,8 @@
 //
 // The columns are fp16 too: fp16 activations as they are; bf16 ones times the power of two that takes a row's largest magnitude to
 // 2^14 .. 2^15. Values down to 2^-29 of the largest keep all their bits then, below that the error is at most 2^-39 of the largest:
-// far under the 2^-24 of each fp32 sum. fp32 values (an expert's hidden values) take two columns, fp16(x) and fp16(x - fp16(x)),
-// scaled the same way: 22 bits.
+// far under the 2^-24 of each fp32 sum. fp32 values (an expert's hidden values) are rounded to fp16 after the same scaling: 11 bits,
+// as an fp16 model keeps them and three more than a bf16 one does.
 //
 // A strip is 16 rows of a record: 4j .. 4j + 3, + 32, + 64, + 96, whose scales are 64 neighbouring bytes for every 128
 // columns. A unit is a strip x 128 columns: 1024 bytes and 64 of scales. The warps of a CTA share a strip's units; each has
@@ -154,19 +154,16 @@ __device__ __forceinline__ uint4 pack_half8(const float* x) {
 
 // Lays this warp's share of the columns out for add_unit: units warp, warp + kFewWarps, ... below `units`, each 128 values from
 // column `from` + 128 u on; values behind `cols` are zeros. Of every block of 32 values column after column, 64 bytes each, so a
-// block is 64 * columns bytes. `sources` rows are read, row_of(i) is the i-th: column i of 16-bit values, columns 2i and 2i + 1 (the
-// values rounded to fp16, and what the rounding left) of 32-bit ones. Each row is scaled by a power of two of the warp's own, whose
-// inverse goes to inverse[column]: no other warp reads these units, and sums are scaled back before they are joined.
+// block is 64 * columns bytes; row_of(i) is where the i-th column's values come from. Each is scaled by a power of two of the
+// warp's own, whose inverse goes to inverse[i]: no other warp reads these units, and sums are scaled back before they are joined.
 template <int DT, class RowOf>
-__device__ __forceinline__ void stage_share(RowOf row_of, uint32_t sources, uint32_t units, uint32_t from, uint32_t cols, uint32_t dst,
+__device__ __forceinline__ void stage_share(RowOf row_of, uint32_t columns, uint32_t units, uint32_t from, uint32_t cols, uint32_t dst,
                                             float* inverse, uint32_t warp, uint32_t lane) {
     constexpr int kElem = DT == ENEC_FP32 ? 4 : 2;
-    constexpr uint32_t kParts = DT == ENEC_FP32 ? 2 : 1;
-    const uint32_t columns = sources * kParts;
     const uint32_t group = lane & 15;   // of eight values in a unit; half a warp takes a row
-    for (uint32_t first = 0; first < sources; first += 2) {
+    for (uint32_t first = 0; first < columns; first += 2) {
         const uint32_t i = first + (lane >> 4);
-        const bool mine = i < sources;
+        const bool mine = i < columns;
         const uint8_t* row = mine ? row_of(i) : nullptr;
         auto load = [&](uint32_t u, float* x) {
             uint32_t w[2 * kElem];
@@ -186,30 +183,15 @@ __device__ __forceinline__ void stage_share(RowOf row_of, uint32_t sources, uint
             for (int d = 1; d < 16; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
         }
         const float factor = DT == ENEC_FP16 ? 1.f : column_factor(top);
-        if (mine && group == 0) {
-#pragma unroll
-            for (uint32_t p = 0; p < kParts; ++p) inverse[i * kParts + p] = DT == ENEC_FP16 ? 1.f : column_inverse(top);
-        }
+        if (mine && group == 0) inverse[i] = DT == ENEC_FP16 ? 1.f : column_inverse(top);
 #pragma unroll 4
         for (uint32_t u = warp; u < units; u += kFewWarps) {
             float x[8];
             load(u, x);
             if (!mine) continue;
-            const uint32_t at = dst + (u * 4 + (group >> 2)) * columns * 64 + i * kParts * 64 + (group & 3) * 16;
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] *= factor;
-            const uint4 high = pack_half8(x);
-            sts128(at, high);
-            if constexpr (kParts == 2) {
-                const uint32_t hw[4] = {high.x, high.y, high.z, high.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 v = MicroType<ENEC_FP16>::unpack(hw[k]);
-                    x[2 * k] = fabsf(v.x) < 65536.f ? x[2 * k] - v.x : 0.f;   // an infinity or a NaN leaves nothing
-                    x[2 * k + 1] = fabsf(v.y) < 65536.f ? x[2 * k + 1] - v.y : 0.f;
-                }
-                sts128(at + 64, pack_half8(x));
-            }
+            sts128(dst + (u * 4 + (group >> 2)) * columns * 64 + i * 64 + (group & 3) * 16, pack_half8(x));
         }
     }
     __syncwarp();

@@ -18,6 +18,7 @@ struct MicroProduct {
 };
 
 constexpr uint32_t kFewMostShared = 227 * 1024;
+constexpr uint32_t kFewHalfShared = 228 * 1024 / 2 - 1024;   // two CTAs on an SM: each has a kilobyte of the system's beside its own
 
 // The most tokens one launch for few tokens takes with rows of `cols` values (32, or fewer where they would not fit; 0 where not one does).
 uint32_t micro_few_most_tokens(uint32_t cols);

@@ -1,0 +1,102 @@
+// tcgen05 in the form the products of many tokens use it: one CTA per tile, accumulators in tensor memory, operands in shared memory,
+// K-major with rows of 128 bytes whose 16-byte chunks are exchanged by the row's number mod 8.
+#pragma once
+
+#include "enec_micro.cuh"
+
+namespace enec {
+
+#ifdef __CUDACC__
+
+__device__ __forceinline__ void tmem_alloc(uint32_t* where, uint32_t columns) {   // by one whole warp
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns) {      // by the warp that has taken it
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tcgen05_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tcgen05_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Arrives on `bar` when all tcgen05 operations that this thread has issued are done.
+__device__ __forceinline__ void tcgen05_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// Descriptor of an operand: address, 1024 bytes from eight rows to the next eight, 128-byte swizzle.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+    return uint64_t((addr & 0x3FFFF) >> 4) | uint64_t(1) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+}
+// Descriptor of 512 bytes of scales: 32 rows of 16 bytes, eight rows after another, no swizzle.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
+    return uint64_t((addr & 0x3FFFF) >> 4) | uint64_t(1) << 16 | uint64_t(128 >> 4) << 32 | uint64_t(1) << 46;
+}
+// Those 512 bytes to four columns of tensor memory, the same for all four groups of 32 lanes.
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+
+// D (128 rows x n columns) (+)= A B^T over 64 columns of E2M1 with one scale per 32.
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(uint32_t(add))
+        : "memory");
+}
+// E2M1 operands (1), E8M0 scales (bit 23), both K-major; the pair of scale bytes in their words goes in at bits 4 (B) and 29 (A).
+__device__ __forceinline__ uint32_t scaled_idesc(uint32_t n) { return 1u << 7 | 1u << 10 | (n >> 3) << 17 | 1u << 23 | 1u << 27; }
+
+// D (128 rows x n columns) (+)= A B^T over 16 columns of bf16 or fp16, fp32 sums.
+__device__ __forceinline__ void mma_16bit(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+        : "memory");
+}
+// fp32 sums (bit 4), bf16 (1) or fp16 (0) operands, both K-major, 128 rows.
+__device__ __forceinline__ uint32_t idesc_16bit(bool bf16, uint32_t n) {
+    return 1u << 4 | uint32_t(bf16) << 7 | uint32_t(bf16) << 10 | (n >> 3) << 17 | (128u >> 4) << 24;
+}
+
+// 16 columns of this warp's 32 lanes of tensor memory.
+__device__ __forceinline__ void tmem_load16(uint32_t tmem, uint32_t* v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+          "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(tmem));
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// Stores a warp's 32 rows (lanes) x 16 tokens (registers) to y[token][row]. Two tokens at a time, neighbouring lanes exchange values
+// so that each stores two rows of one token: 4 bytes a lane instead of 2. `wide`: y and its rows lie on 4-byte boundaries.
+template <int DT>
+__device__ __forceinline__ void store_tile16(uint8_t* y, uint64_t ld_y, uint32_t token, uint32_t tokens, uint32_t row, uint32_t rows,
+                                             const uint32_t* v, float factor, bool wide, uint32_t lane) {
+    using T = typename MicroType<DT>::T;
+#pragma unroll
+    for (int j = 0; j < 16; j += 2) {
+        const float a = __uint_as_float(v[j]) * factor, b = __uint_as_float(v[j + 1]) * factor;
+        const float theirs = __shfl_xor_sync(0xFFFFFFFFu, lane & 1 ? a : b, 1);
+        const uint32_t to = token + j + (lane & 1);
+        const uint32_t first = row & ~1u;    // of the two rows that this lane stores
+        const float low = lane & 1 ? theirs : a, high = lane & 1 ? b : theirs;
+        if (to < tokens) {
+            T* at = reinterpret_cast<T*>(y) + uint64_t(to) * ld_y + first;
+            if (wide && first + 1 < rows) {
+                *reinterpret_cast<uint32_t*>(at) = MicroType<DT>::pack(low, high);
+            } else {
+                if (first < rows) at[0] = MicroType<DT>::one(low);
+                if (first + 1 < rows) at[1] = MicroType<DT>::one(high);
+            }
+        }
+    }
+}
+
+#endif  // __CUDACC__
+
+}  // namespace enec

@@ -70,12 +70,14 @@ def stream(x):
     return out
 
 
-def layer(x, router, gate, up, down, top, renormalize):
-    """The expert layer; gate, up [experts, inter, hidden] and down [experts, hidden, inter] as values. Also the chosen experts."""
+def layer(x, router, gate, up, down, top, renormalize, chosen=None):
+    """The expert layer; gate, up [experts, inter, hidden] and down [experts, hidden, inter] as values. Also the chosen experts, which
+    are the largest logits' unless they are given."""
     logits = x @ router.T
     p = np.exp(logits - logits.max(-1, keepdims=True))
     p /= p.sum(-1, keepdims=True)
-    chosen = np.argsort(-logits, axis=-1, kind="stable")[:, :top]
+    if chosen is None:
+        chosen = np.argsort(-logits, axis=-1, kind="stable")[:, :top]
     y = np.zeros_like(x)
     for t in range(x.shape[0]):
         w = p[t, chosen[t]]

@@ -85,3 +85,41 @@ def test_dequantize_refuses(lib, changed, want):
     (dict(tokens=0), OK), (dict(rows=0), OK)])
 def test_matmul_refuses_or_has_nothing_to_do(lib, changed, want):
     assert matmul(lib, **changed) == want
+
+
+def both(lib, d_x=P, x_size=1 << 20, tokens=4, d_w=P, w_size=1 << 20, rows=8, cols=64, dt=0, d_y=P, ld_y=8):
+    return lib.enec_matmul_microscaled_both(d_x, x_size, tokens, d_w, w_size, rows, cols, dt, d_y, ld_y, None, None)
+
+
+@pytest.mark.parametrize("changed, want", [
+    (dict(dt=2), DTYPE), (dict(dt=5), DTYPE), (dict(d_x=None), INVALID), (dict(d_w=None), INVALID), (dict(d_y=None), INVALID),
+    (dict(d_x=P + 2), INVALID), (dict(d_w=P + 8), INVALID), (dict(d_y=P + 2), INVALID), (dict(ld_y=7), INVALID), (dict(ld_y=1 << 36), INVALID),
+    (dict(x_size=17408), SMALL), (dict(w_size=17408), SMALL), (dict(tokens=129, x_size=128 + 17408), SMALL), (dict(rows=1 << 31, ld_y=1 << 31), LARGE),
+    (dict(tokens=1 << 31), LARGE), (dict(tokens=0), OK), (dict(rows=0), OK)])
+def test_both_refuses_or_has_nothing_to_do(lib, changed, want):
+    assert both(lib, **changed) == want
+
+
+def moe(lib, d_x=P, dt=0, tokens=4, hidden=64, ld_x=64, d_router=P, experts=8, top=2, renormalize=1, d_gate=P, gate=1 << 20, d_up=P, up=1 << 20,
+        d_down=P, down=1 << 20, inter=32, d_y=P, ld_y=64, d_workspace=P, workspace=1 << 20):
+    return lib.enec_moe_microscaled(d_x, dt, tokens, hidden, ld_x, d_router, experts, top, renormalize, d_gate, gate, d_up, up, d_down, down, inter,
+                                    d_y, ld_y, d_workspace, workspace, None, None)
+
+
+@pytest.mark.parametrize("changed, want", [
+    (dict(dt=2), DTYPE), (dict(tokens=65), LARGE), (dict(experts=513), LARGE), (dict(top=17), LARGE), (dict(tokens=64, experts=385), LARGE),
+    (dict(hidden=1 << 24, ld_x=1 << 24, ld_y=1 << 24), LARGE), (dict(inter=1 << 24), LARGE),
+    (dict(top=0), INVALID), (dict(top=9), INVALID), (dict(experts=0), INVALID), (dict(hidden=0), INVALID), (dict(inter=0), INVALID),
+    (dict(ld_x=63), INVALID), (dict(ld_y=63), INVALID), (dict(gate=128 + 8 * 17408 - 1), SMALL), (dict(up=0), SMALL), (dict(down=17408), SMALL),
+    (dict(workspace=64), SMALL), (dict(tokens=0), OK)]
+    + [({name: bad}, INVALID) for name in ("d_x", "d_router", "d_gate", "d_up", "d_down", "d_y", "d_workspace") for bad in (None, P + 8)])
+def test_moe_refuses_or_has_nothing_to_do(lib, changed, want):
+    assert moe(lib, **changed) == want
+
+
+def test_moe_workspace_holds_the_pairs_values(lib):
+    f = lib.enec_moe_microscaled_workspace
+    assert f(65, 64, 32, 8, 2) == 0 and f(4, 64, 32, 513, 2) == 0
+    for tokens, hidden, inter, experts, top in ((1, 1, 1, 1, 1), (4, 64, 32, 8, 2), (64, 2048, 1408, 64, 6)):
+        pairs = tokens * top
+        assert f(tokens, hidden, inter, experts, top) >= pairs * (hidden + inter) * 4 + pairs * 8
