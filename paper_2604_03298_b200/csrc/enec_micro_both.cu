@@ -129,6 +129,7 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
                 tcgen05_commit(empty + s);
             }
             tcgen05_commit(&done);
+            mbar_wait_bounded(&done, 0);   // no instruction may be under way when tensor memory is given back
         }
     } else {
         const bool good = micro_header_ok(job.w, job.sw) && micro_header_ok(job.x, job.sx);

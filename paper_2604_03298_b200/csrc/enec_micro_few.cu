@@ -154,15 +154,15 @@ uint32_t micro_few_most_tokens(uint32_t cols) {
     return 0;
 }
 
-enec_status micro_few(const MicroProduct& p, uint32_t first, uint32_t tokens, const MicroDevice& dev, cudaStream_t stream) {
+enec_status micro_few(const MicroProduct& p, const MicroDevice& dev, cudaStream_t stream) {
     FewJob job;
-    job.x = p.x + uint64_t(first) * p.ld_x * 2;
+    job.x = p.x;
     job.ld_x = p.ld_x;
     job.w = p.w;
     job.s = p.s;
-    job.y = p.y + uint64_t(first) * p.ld_y * 2;
+    job.y = p.y;
     job.ld_y = p.ld_y;
-    job.tokens = tokens;
+    job.tokens = p.tokens;
     const uint32_t last = p.s.rows - (p.s.row_tiles - 1) * kMicroRows;   // rows of the last record
     job.strips = (p.s.row_tiles - 1) * 8 + (last >= 32 ? 8 : (last + 3) / 4);
     job.status = p.status;

@@ -22,7 +22,8 @@ constexpr uint32_t kFewHalfShared = 228 * 1024 / 2 - 1024;   // two CTAs on an S
 
 // The most tokens one launch for few tokens takes with rows of `cols` values (32, or fewer where they would not fit; 0 where not one does).
 uint32_t micro_few_most_tokens(uint32_t cols);
-// Tokens first .. first + tokens - 1 of the product.
-enec_status micro_few(const MicroProduct& p, uint32_t first, uint32_t tokens, const MicroDevice& dev, cudaStream_t stream);
+enec_status micro_few(const MicroProduct& p, const MicroDevice& dev, cudaStream_t stream);
+// All tokens of the product, on the tensor cores.
+enec_status micro_many(const MicroProduct& p, const MicroDevice& dev, cudaStream_t stream);
 
 }  // namespace enec

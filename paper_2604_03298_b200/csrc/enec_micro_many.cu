@@ -1,0 +1,409 @@
+// y = x W^T for many tokens, W a microscaled stream, x of 16 bits: tcgen05.mma (kind::f16) on weights that are brought back on the way.
+//
+// Lanes of the accumulator are rows of W, its columns tokens: 256 (two accumulators) or 128 rows x up to 256 tokens a CTA. Of 64 columns
+// (a step) the tensor cores take 1024 clocks at 256 x 256. Meanwhile eight warps turn 16384 codes into 16-bit values in shared
+// memory (5 instructions a pair, some 370 clocks of the SM's issue slots) and four warps fetch 32 KB of x with cp.async, 32 bytes a
+// clock from L2; tiles of 128 x 256 would need twice that, more than L2 gives to all SMs at a time. Raw records are copied in bulk; a
+// thread takes its share of a record to registers at once, so that one record's room is enough.
+//
+// bf16: a code's value times its scale is exact in bf16 over the whole range of scales. fp16: it would not be, so a row's values are
+// held times 2^-(largest scale exponent of the row), and the sum is scaled back: what is lost lies under 2^-24 of the row's largest.
+//
+// Where the tiles would not fill the SMs, a cluster of CTAs shares the columns: each leaves its sums in its shared memory and adds
+// up a part of the tokens, in the order of the CTAs.
+#include "enec_micro_mma.cuh"
+
+#include <cooperative_groups.h>
+
+#include "enec_micro_launch.cuh"
+
+namespace enec {
+namespace {
+
+constexpr uint32_t kManyThreads = 14 * 32;   // bulk copies, matrix instructions, 4 warps for x, 8 for the weights and the results
+constexpr uint32_t kFirstX = 2, kFirstW = 6;
+constexpr uint32_t kStagesA = 2, kStagesB = 3;
+constexpr uint32_t kManyMostTokens = 256;
+
+struct ManyJob {
+    const uint8_t* x;
+    uint64_t ld_x;
+    const uint8_t* w;
+    MicroShape s;
+    uint8_t* y;
+    uint64_t ld_y;
+    uint32_t tokens;
+    uint32_t tile_tokens;    // a multiple of 16
+    uint32_t row_tiles;      // tiles along the rows
+    uint32_t cluster;        // CTAs that share a tile's columns
+    uint32_t share;          // records of columns each takes
+    uint32_t aligned;        // rows of x begin on 16-byte boundaries
+    int* status;
+};
+
+template <int MT>
+__host__ __device__ constexpr uint32_t many_bytes(uint32_t tokens) {
+    return MT * kMicroRecordBytes + kStagesA * MT * 16384 + kStagesB * tokens * 128 + 1024;
+}
+
+__device__ __forceinline__ void cp_async16_some(uint32_t dst, const void* src, uint32_t bytes) {   // the rest of the 16 are zeros
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ uint32_t bf16_times(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 r = __hmul2(reinterpret_cast<const __nv_bfloat162&>(a), reinterpret_cast<const __nv_bfloat162&>(b));
+    return reinterpret_cast<const uint32_t&>(r);
+}
+__device__ __forceinline__ uint32_t fp16_times(uint32_t a, uint32_t b) {
+    const __half2 r = __hmul2(reinterpret_cast<const __half2&>(a), reinterpret_cast<const __half2&>(b));
+    return reinterpret_cast<const uint32_t&>(r);
+}
+
+// Eight codes times 2^(byte - 127) in bf16. fp16 holds a code's value with its exponent field in 14 .. 17 and at most one mantissa bit;
+// the same fields three bits further down are the value times 2^-112 in bf16.
+__device__ __forceinline__ uint4 to_bf16(uint32_t codes, uint32_t byte) {
+    const uint4 h = e2m1_values(codes);
+    uint32_t v[4] = {h.x, h.y, h.z, h.w};
+    const uint32_t one = byte == 255 ? 0x7FC0u : (min(byte, 142u) + 112) << 7;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = bf16_times((v[i] & 0x80008000u) | ((v[i] >> 3) & 0x0FFF0FFFu), one * 0x10001u);
+    if (byte > 142 && byte < 255) {   // scales above 2^15
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = bf16_times(v[i], ((byte - 142 + 127) << 7) * 0x10001u);
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+// Eight codes times 2^(byte - top), byte <= top, in fp16.
+__device__ __forceinline__ uint4 to_fp16(uint32_t codes, uint32_t byte, uint32_t top) {
+    const uint4 h = e2m1_values(codes);
+    const uint32_t below = top - byte;
+    const uint32_t one = byte == 255 ? 0x7E00u : below < 15 ? (15 - below) << 10 : below < 25 ? 0x400u >> (below - 14) : 0u;
+    const uint32_t f = one * 0x10001u;
+    return make_uint4(fp16_times(h.x, f), fp16_times(h.y, f), fp16_times(h.z, f), fp16_times(h.w, f));
+}
+
+template <int DT, int MT>
+__global__ void __launch_bounds__(kManyThreads, MT == 1 ? 2 : 1) enec_micro_many_kernel(const __grid_constant__ ManyJob job) {
+    extern __shared__ uint8_t raw_shared[];
+    __shared__ uint64_t raw_full, raw_empty, full_a[kStagesA], empty_a[kStagesA], full_b[kStagesB], empty_b[kStagesB], done;
+    __shared__ uint32_t tmem_at;
+    __shared__ volatile int failed;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t* smem = raw_shared + ((1024 - (smem_u32(raw_shared) & 1023)) & 1023);
+    const uint32_t n = job.tile_tokens;
+    uint32_t tmem_columns = 32;
+    while (tmem_columns < MT * n) tmem_columns *= 2;
+    if (threadIdx.x == 0) {
+        mbar_init(&raw_full, 1);
+        mbar_init(&raw_empty, 256);
+        for (uint32_t i = 0; i < kStagesA; ++i) mbar_init(full_a + i, 256), mbar_init(empty_a + i, 1);
+        for (uint32_t i = 0; i < kStagesB; ++i) mbar_init(full_b + i, 128), mbar_init(empty_b + i, 1);
+        mbar_init(&done, 1);
+        mbar_fence_init();
+        failed = 0;
+    }
+    if (warp == 1) tmem_alloc(&tmem_at, tmem_columns);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_at;
+    pdl_wait();
+    pdl_launch_dependents();
+
+    const uint32_t rank = job.cluster > 1 ? blockIdx.x % job.cluster : 0, tile = blockIdx.x / job.cluster;
+    const uint32_t row_tile = tile % job.row_tiles * MT, token0 = tile / job.row_tiles * n;
+    const uint32_t mt = min(uint32_t(MT), job.s.row_tiles - row_tile);
+    const uint32_t k0 = min(rank * job.share, job.s.col_tiles), k1 = min(k0 + job.share, job.s.col_tiles);
+    const uint32_t records = k1 - k0;
+    const uint32_t columns = min(job.s.cols, k1 * kMicroCols) - min(job.s.cols, k0 * kMicroCols);
+    const uint32_t steps = (columns + 63) / 64;
+    const uint64_t strip = uint64_t(job.s.col_tiles) * kMicroRecordBytes;
+    const uint8_t* wr = job.w + kMicroHeaderBytes + row_tile * strip + uint64_t(k0) * kMicroRecordBytes;
+    uint8_t* a_ring = smem;
+    uint8_t* b_ring = a_ring + kStagesA * MT * 16384;
+    uint8_t* raw = b_ring + kStagesB * n * 128;
+    const bool good = micro_header_ok(job.w, job.s);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t k = 0;
+            for (; k < records; ++k) {
+                if (k > 0 && !suspended_wait(&raw_empty, (k - 1) & 1, const_cast<volatile int*>(&failed))) {
+                    failed = 1;
+                    break;
+                }
+                mbar_expect_tx(&raw_full, mt * kMicroRecordBytes);
+                for (uint32_t i = 0; i < mt; ++i)
+                    bulk_g2s(raw + i * kMicroRecordBytes, wr + i * strip + uint64_t(k) * kMicroRecordBytes, kMicroRecordBytes, &raw_full);
+            }
+            if (k > 0) mbar_wait_bounded(&raw_full, (k - 1) & 1);   // nothing may be in flight when the CTA ends
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = idesc_16bit(DT == ENEC_BF16, n);
+            for (uint32_t j = 0; j < steps; ++j) {
+                const uint32_t sa = j % kStagesA, sb = j % kStagesB;
+                if (!suspended_wait(full_a + sa, (j / kStagesA) & 1, &failed) || !suspended_wait(full_b + sb, (j / kStagesB) & 1, &failed)) {
+                    failed = 1;
+                    break;
+                }
+                tcgen05_fence_after();
+                const uint32_t a = smem_u32(a_ring) + sa * MT * 16384, b = smem_u32(b_ring) + sb * n * 128;
+#pragma unroll
+                for (uint32_t i = 0; i < MT; ++i) {
+                    if (i < mt) {
+#pragma unroll
+                        for (uint32_t q = 0; q < 4; ++q)
+                            mma_16bit(tmem + i * n, operand_desc(a + i * 16384 + q * 32), operand_desc(b + q * 32), idesc, j > 0 || q > 0);
+                    }
+                }
+                tcgen05_commit(empty_a + sa);
+                tcgen05_commit(empty_b + sb);
+            }
+            tcgen05_commit(&done);
+            mbar_wait_bounded(&done, 0);   // no instruction may be under way when tensor memory is given back
+        }
+    } else if (warp < kFirstW) {
+        // x: eight lanes a row of 64 columns
+        const uint32_t me = threadIdx.x - kFirstX * 32, c = me & 7;
+        const uint32_t first_col = min(k0 * kMicroCols, job.s.cols);
+        uint32_t waiting = 0;   // steps asked for and not announced
+        uint32_t announced = 0;
+        auto announce = [&]() {
+            fence_async_shared();
+            mbar_arrive(full_b + announced % kStagesB);
+            ++announced;
+            --waiting;
+        };
+        bool ok = true;
+        for (uint32_t j = 0; j < steps; ++j) {
+            const uint32_t sb = j % kStagesB;
+            if (j >= kStagesB && !suspended_wait(empty_b + sb, (j / kStagesB - 1) & 1, &failed)) {
+                ok = false;
+                break;
+            }
+            const uint32_t dst = smem_u32(b_ring) + sb * n * 128;
+            const uint32_t col = j * 64 + c * 8;                                     // of this CTA's columns
+            const uint32_t valid = col < columns ? min(columns - col, 8u) : 0;
+            if (job.aligned) {
+                const uint8_t* from = job.x + (uint64_t(token0) * job.ld_x + first_col + (valid ? col : 0)) * 2;
+#pragma unroll 4
+                for (uint32_t r = me >> 3; r < n; r += 16) {
+                    const bool real = token0 + r < job.tokens;
+                    cp_async16_some(dst + r * 128 + ((c ^ (r & 7)) << 4), from + (real ? uint64_t(r) * job.ld_x * 2 : 0), real ? valid * 2 : 0);
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                ++waiting;
+                if (waiting == 2) {   // the step before this one has arrived while this one is on its way
+                    asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    announce();
+                }
+            } else {
+                const uint8_t* from = job.x + (uint64_t(token0) * job.ld_x + first_col + col) * 2;
+                for (uint32_t r0 = me >> 3; r0 < n; r0 += 64) {
+                    uint32_t v[4][4];
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        const uint32_t r = r0 + 16 * i;
+                        load_eight<DT>(from + uint64_t(r) * job.ld_x * 2, r < n && token0 + r < job.tokens ? int(valid) : 0, v[i]);
+                    }
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        const uint32_t r = r0 + 16 * i;
+                        if (r < n) sts128(dst + r * 128 + ((c ^ (r & 7)) << 4), make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]));
+                    }
+                }
+                ++waiting;
+                announce();
+            }
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        while (waiting) announce();
+        if (!ok) failed = 1;
+    } else {
+        // the weights: thread (row, half) brings back 32 of the 64 columns of a step, of one row in each 128
+        const uint32_t me = threadIdx.x - kFirstW * 32, r = me & 127, half = me >> 7;
+        uint32_t top[MT];
+        if constexpr (DT == ENEC_FP16) {
+#pragma unroll
+            for (uint32_t i = 0; i < MT; ++i) {
+                uint32_t most = 0;   // the largest of the row's scale bytes, four at a time; 255 does not count
+                const uint8_t* at = wr + i * strip + kMicroElemBytes + (r & 31) * 16 + (r >> 5) * 4;
+                if (i < mt) {
+#pragma unroll 8
+                    for (uint32_t b = 0; b < 2 * records; ++b) {
+                        const uint32_t four = __ldg(reinterpret_cast<const uint32_t*>(at + uint64_t(b >> 1) * kMicroRecordBytes + (b & 1) * 512));
+                        most = __vmaxu4(most, four & ~__vcmpeq4(four, 0xFFFFFFFFu));
+                    }
+                }
+                most = max(max(most & 255, most >> 8 & 255), max(most >> 16 & 255, most >> 24));
+                top[i] = most;
+            }
+        }
+        bool ok = true;
+        for (uint32_t k = 0; k < records && ok; ++k) {
+            if (!suspended_wait(&raw_full, k & 1, &failed)) {
+                ok = false;
+                break;
+            }
+            uint4 codes[MT][4];
+            uint2 scales[MT];   // eight bytes
+#pragma unroll
+            for (uint32_t i = 0; i < MT; ++i) {
+                if (i >= mt) continue;
+                const uint32_t rec = smem_u32(raw) + i * kMicroRecordBytes;
+#pragma unroll
+                for (uint32_t q = 0; q < 4; ++q) codes[i][q] = lds128(rec + r * 128 + (((2 * q + half) ^ (r & 7)) << 4));
+                const uint32_t at = rec + kMicroElemBytes + (r & 31) * 16 + (r >> 5) * 4;
+                scales[i] = make_uint2(lds32(at), lds32(at + 512));
+            }
+            mbar_arrive(&raw_empty);
+            const uint32_t here = min(4u, steps - 4 * k);
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                if (q >= here) break;
+                const uint32_t j = 4 * k + q, sa = j % kStagesA;
+                if (j >= kStagesA && !suspended_wait(empty_a + sa, (j / kStagesA - 1) & 1, &failed)) {
+                    ok = false;
+                    break;
+                }
+#pragma unroll
+                for (uint32_t i = 0; i < MT; ++i) {
+                    if (i >= mt) continue;
+                    const uint32_t word = q < 2 ? scales[i].x : scales[i].y;
+                    const uint32_t byte = word >> (8 * (2 * (q & 1) + half)) & 255;
+                    const uint32_t dst = smem_u32(a_ring) + (sa * MT + i) * 16384 + r * 128;
+                    const uint32_t w[4] = {codes[i][q].x, codes[i][q].y, codes[i][q].z, codes[i][q].w};
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e)
+                        sts128(dst + (((4 * half + e) ^ (r & 7)) << 4), DT == ENEC_BF16 ? to_bf16(w[e], byte) : to_fp16(w[e], byte, top[i]));
+                }
+                fence_async_shared();
+                mbar_arrive(full_a + sa);
+            }
+        }
+        if (!ok) failed = 1;
+        if (!suspended_wait(&done, 0, &failed)) failed = 1;
+        tcgen05_fence_after();
+        // results: the warp's quarter of the lanes, every other 16 tokens
+        const uint32_t quarter = warp & 3, group = (warp - kFirstW) >> 2;
+        const uint32_t row_in = quarter * 32 + lane;
+        const bool wide = (job.ld_y & 1) == 0;
+        float factor[MT];
+#pragma unroll
+        for (uint32_t i = 0; i < MT; ++i) factor[i] = 1.f;
+        if constexpr (DT == ENEC_FP16) {
+            // the rows' exponents change hands through shared memory that no operand uses any more
+            uint8_t* tops = smem;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+#pragma unroll
+            for (uint32_t i = 0; i < MT; ++i)
+                if (half == 0) tops[i * 128 + r] = uint8_t(top[i]);
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+#pragma unroll
+            for (uint32_t i = 0; i < MT; ++i) factor[i] = micro_scale(tops[i * 128 + row_in]);
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+        }
+        if (!failed && steps > 0) {
+            for (uint32_t i = 0; i < mt; ++i) {
+                const uint32_t row = (row_tile + i) * kMicroRows + row_in;
+                for (uint32_t c = group * 16; c < n; c += 32) {
+                    if (token0 + c >= job.tokens) break;
+                    uint32_t v[16];
+                    tmem_load16(tmem + (quarter * 32 << 16) + i * n + c, v);
+                    tmem_load_wait();
+                    if (MT == 1 && job.cluster > 1) {
+                        float* sums = reinterpret_cast<float*>(smem);   // [token][row]
+#pragma unroll
+                        for (uint32_t e = 0; e < 16; ++e) sums[(c + e) * kMicroRows + row_in] = __uint_as_float(v[e]) * factor[i];
+                    } else if (good) {
+                        store_tile16<DT>(job.y, job.ld_y, token0 + c, job.tokens, row, job.s.rows, v, factor[i], wide, lane);
+                    }
+                }
+            }
+        }
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    if (threadIdx.x == 0) {
+        if (failed) report(job.status, ENEC_ERR_TIMEOUT);
+        else if (!good && blockIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
+    }
+    if (warp == 1) tmem_free(tmem, tmem_columns);
+    if constexpr (MT == 1) {
+        if (job.cluster > 1) {
+            // CTAs that have columns have left their sums; each adds up every cluster-th group of 4 tokens
+            using T = typename MicroType<DT>::T;
+            auto cluster = cooperative_groups::this_cluster();
+            cluster.sync();
+            const uint32_t with = (job.s.col_tiles + job.share - 1) / job.share;
+            const uint32_t row_in = threadIdx.x & 127;
+            const uint32_t row = row_tile * kMicroRows + row_in;
+            if (threadIdx.x < 384 && good && !failed && row < job.s.rows) {
+                for (uint32_t t = (threadIdx.x >> 7) * job.cluster + rank; t < n && token0 + t < job.tokens; t += 3 * job.cluster) {
+                    float v = 0.f;
+                    for (uint32_t k = 0; k < with; ++k)
+                        v += cluster.map_shared_rank(reinterpret_cast<float*>(smem), k)[t * kMicroRows + row_in];
+                    reinterpret_cast<T*>(job.y)[uint64_t(token0 + t) * job.ld_y + row] = MicroType<DT>::one(v);
+                }
+            }
+            cluster.sync();   // no CTA ends while its sums are read
+        }
+    }
+}
+
+template <int DT, int MT>
+enec_status launch_many(const ManyJob& job, uint32_t tiles, const MicroDevice& dev, cudaStream_t stream) {
+    static std::atomic<uint64_t> allowed{0};
+    if (!allow_shared(allowed, dev, enec_micro_many_kernel<DT, MT>, many_bytes<MT>(kManyMostTokens))) return ENEC_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(tiles * job.cluster);
+    cfg.blockDim = dim3(kManyThreads);
+    cfg.dynamicSmemBytes = many_bytes<MT>(job.tile_tokens);
+    if (job.cluster > 1 && cfg.dynamicSmemBytes < job.tile_tokens * kMicroRows * 4 + 1024) cfg.dynamicSmemBytes = job.tile_tokens * kMicroRows * 4 + 1024;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = job.cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = job.cluster > 1 ? 2 : 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, enec_micro_many_kernel<DT, MT>, job);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return err == cudaSuccess ? ENEC_OK : ENEC_ERR_CUDA;
+}
+
+}  // namespace
+
+enec_status micro_many(const MicroProduct& p, const MicroDevice& dev, cudaStream_t stream) {
+    ManyJob job;
+    job.x = p.x;
+    job.ld_x = p.ld_x;
+    job.w = p.w;
+    job.s = p.s;
+    job.y = p.y;
+    job.ld_y = p.ld_y;
+    job.tokens = p.tokens;
+    job.aligned = p.ld_x % 8 == 0;
+    job.status = p.status;
+    const uint64_t token_tiles = (p.tokens + kManyMostTokens - 1) / kManyMostTokens;
+    job.tile_tokens = uint32_t(((p.tokens + token_tiles - 1) / token_tiles + 15) / 16 * 16);
+    // 256 rows a tile where that leaves work for most SMs; else 128, and the columns shared out while more than one tile an SM is missing
+    uint32_t mt = 2;
+    uint64_t tiles = (p.s.row_tiles + 1) / 2 * token_tiles;
+    if (tiles * 4 < uint64_t(dev.sms) * 3) mt = 1, tiles = p.s.row_tiles * token_tiles;
+    if (tiles >> 28) return ENEC_ERR_TOO_LARGE;
+    job.row_tiles = (p.s.row_tiles + mt - 1) / mt;
+    job.cluster = 1;
+    if (mt == 1)
+        while (job.cluster < 8 && tiles * job.cluster * 2 <= uint64_t(dev.sms) * 3 / 2 && p.s.col_tiles >= 4 * job.cluster) job.cluster *= 2;
+    job.share = (p.s.col_tiles + job.cluster - 1) / job.cluster;
+    if (p.dt == ENEC_BF16)
+        return mt == 2 ? launch_many<ENEC_BF16, 2>(job, uint32_t(tiles), dev, stream) : launch_many<ENEC_BF16, 1>(job, uint32_t(tiles), dev, stream);
+    return mt == 2 ? launch_many<ENEC_FP16, 2>(job, uint32_t(tiles), dev, stream) : launch_many<ENEC_FP16, 1>(job, uint32_t(tiles), dev, stream);
+}
+
+}  // namespace enec

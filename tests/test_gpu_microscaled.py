@@ -175,6 +175,12 @@ def test_product_of_small_and_large_activations(tokens, scale):
 
 
 @pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("tokens, rows, cols, gap", [(2000, 4096, 320, 0), (1500, 5000, 257, 1), (2047, 3969, 64, 8), (257, 16500, 100, 0)])
+def test_product_of_many_tiles(dt, tokens, rows, cols, gap):
+    check_product(tokens, rows, cols, dt, gap)
+
+
+@pytest.mark.parametrize("dt", [0, 1])
 @pytest.mark.parametrize("tokens, rows, cols", [(8, 48, 14336), (32, 40, 14336), (3, 20, 60000), (1, 4096, 4096), (65, 20, 20000)])
 def test_product_of_long_rows(dt, tokens, rows, cols):
     check_product(tokens, rows, cols, dt)
