@@ -9,33 +9,50 @@
 // operand in shared memory or tensor memory first, one store and one load for each value more. The scale is applied to the inner
 // sum in fp32, so it is exact whatever its size; fp16 holds every E2M1 value exactly.
 //
-// The columns are fp16 too: fp16 activations as they are; bf16 ones times the power of two that takes a row's largest magnitude to
-// 2^14 .. 2^15. Values down to 2^-29 of the largest keep all their bits then, below that the error is at most 2^-39 of the largest:
-// far under the 2^-24 of each fp32 sum. fp32 values (an expert's hidden values) are rounded to fp16 after the same scaling: 11 bits,
-// as an fp16 model keeps them and three more than a bf16 one does.
+// The columns are fp16 too: fp16 activations as they are; bf16 ones times the power of two that takes the largest magnitude of 128
+// neighbouring values to 2^14 .. 2^15. Values down to 2^-29 of the largest keep all their bits then, below that the error is at
+// most 2^-39 of the largest: far under the 2^-24 of each fp32 sum. fp32 values (an expert's hidden values) are rounded to fp16 after
+// the same scaling: 11 bits, as an fp16 model keeps them and three more than a bf16 one does.
 //
 // A strip is 16 rows of a record: 4j .. 4j + 3, + 32, + 64, + 96, whose scales are 64 neighbouring bytes for every 128
-// columns. A unit is a strip x 128 columns: 1024 bytes and 64 of scales. The warps of a CTA share a strip's units; each has
-// a ring of its own in shared memory that it fills with cp.async and reads with ldmatrix, without a barrier among warps, and which
-// goes on from strip to strip while sums are joined.
+// columns. A unit is a strip x 128 columns: 1024 bytes and 64 of scales. A CTA has 16 warps (what hides a unit's chain of copy,
+// ldmatrix, conversion and products is other warps: with 8 on an SM, 8 tokens x 4096 x 14336 took 32 us), in teams of 4, 8 or 16. A
+// team's warps share a strip's units, its sums are joined in shared memory. Each warp has a ring of its own that it fills with
+// cp.async and reads with ldmatrix, without a barrier among warps, and which goes on from strip to strip while sums are joined.
 #pragma once
 
 #include "enec_micro.cuh"
 
 namespace enec {
 
-constexpr uint32_t kFewWarps = 8;
+constexpr uint32_t kFewWarps = 16;
 constexpr uint32_t kFewThreads = kFewWarps * 32;
 constexpr uint32_t kUnitCols = 128;
 constexpr uint32_t kUnitBytes = 16 * 64;
 constexpr uint32_t kUnitScales = 64;
-constexpr uint32_t kFewStages = 6;
 
+__host__ __device__ constexpr uint32_t few_stages(int mats) { return mats == 2 ? 3 : 4; }
 __host__ __device__ constexpr uint32_t few_stage_bytes(int mats) { return mats * (kUnitBytes + kUnitScales); }
-__host__ __device__ constexpr uint32_t few_ring_bytes(int mats) { return kFewWarps * kFewStages * few_stage_bytes(mats); }
-// Warps' sums of a strip, two sets: rows of 8 NT columns and a gap of 4 words against bank conflicts.
+__host__ __device__ constexpr uint32_t few_ring_bytes(int mats) { return kFewWarps * few_stages(mats) * few_stage_bytes(mats); }
+// Warps' sums of a strip: rows of 8 NT columns and a gap of 4 words against bank conflicts.
 __host__ __device__ constexpr uint32_t few_sum_row(int nt) { return 8 * nt + 4; }
-__host__ __device__ constexpr uint32_t few_sum_bytes(int nt, int mats) { return 2 * kFewWarps * mats * 16 * few_sum_row(nt) * 4; }
+__host__ __device__ constexpr uint32_t few_sum_words(int nt, int mats) { return mats * 16 * few_sum_row(nt); }   // of a warp
+__host__ __device__ constexpr uint32_t few_fixed_bytes(int nt, int mats) { return few_ring_bytes(mats) + kFewWarps * few_sum_words(nt, mats) * 4; }
+// The staged columns of a unit: 128 values of fp16 each, and room for the inverses of 8 NT factors.
+__host__ __device__ constexpr uint32_t few_unit_bytes(int nt, uint32_t columns) { return columns * kUnitCols * 2 + 8 * nt * 4; }
+
+// Warps of a team: the split that leaves the fewest warps without work, over strips (of which `ctas` CTAs work at the same time) and
+// over a strip's units. strips 256, 896 and 8016 of 32 units on 148 SMs: 8, 16 and 4.
+inline uint32_t few_team(uint64_t strips, uint32_t units, uint32_t ctas) {
+    uint32_t best = 16;
+    double most = 0;
+    for (uint32_t team : {4u, 8u, 16u}) {
+        const uint64_t teams = uint64_t(ctas) * (kFewWarps / team);
+        const double busy = double(strips) / double((strips + teams - 1) / teams * teams) * units / ((units + team - 1) / team * team);
+        if (busy > most * 1.02) most = busy, best = team;
+    }
+    return best;
+}
 
 #ifdef __CUDACC__
 
@@ -65,23 +82,22 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t two_bytes) {
     return d;
 }
 
-// Asks for one unit: columns 128 u .. of strip j of the records of a row tile, which begin at `records`.
+// Asks for unit u of strip j of the records of a row tile, which begin at `records`. Row m of the strip is row 4j + m mod 4 + 32 (m / 4)
+// of the record: its chunks are exchanged by (m mod 4) + 4 (j mod 2), and in the stage, where rows are 64 bytes, by (m / 2) mod 4.
 __device__ __forceinline__ void ask_unit(const uint8_t* records, uint32_t j, uint32_t u, uint32_t stage, uint32_t lane) {
-    const uint8_t* rec = records + uint64_t(u >> 1) * kMicroRecordBytes;
-    const uint32_t half = u & 1;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t m = (lane >> 2) + 8 * i, c = lane & 3;   // row of the strip, chunk of the unit
-        const uint32_t r = 4 * j + (m & 3) + 32 * (m >> 2);
-        cp_async16(stage + m * 64 + ((c ^ ((m >> 1) & 3)) << 4), rec + r * 128 + (((4 * half + c) ^ (r & 7)) << 4));
-    }
-    if (lane < 4) cp_async16(stage + kUnitBytes + 16 * lane, rec + kMicroElemBytes + half * 512 + (4 * j + lane) * 16);
+    const uint8_t* rec = records + uint64_t(u >> 1) * kMicroRecordBytes + j * 512;
+    const uint32_t m = lane >> 2, c = lane & 3;
+    const uint32_t from = ((m & 3) + 32 * (m >> 2)) * 128 + (((c ^ (m & 3)) << 4) ^ (((j ^ u) & 1) << 6));
+    const uint32_t to = stage + m * 64 + ((c ^ ((m >> 1) & 3)) << 4);
+    cp_async16(to, rec + from);
+    cp_async16(to + 512, rec + from + 8192);   // row m + 8
+    if (lane < 4) cp_async16(stage + kUnitBytes + 16 * lane, rec + kMicroElemBytes + (u & 1) * 512 - j * 448 + 16 * lane);
 }
 
-// Adds one unit's products to acc. columns: the address of the unit's first block in the staged columns (see stage_share), this
-// lane's column and quarter added; a block is `block_bytes` long; lane's column n of tile nt exists where nt < tiles.
+// Adds one unit's products to acc. values: the address of the unit's staged columns (see stage_columns), this lane's column and
+// quarter added; factors: of its columns' inverse factors, 2 (lane mod 4) added. This lane's column n of tile nt exists where exists[nt].
 template <int NT>
-__device__ __forceinline__ void add_unit(float (*acc)[4], uint32_t stage, uint32_t columns, uint32_t block_bytes, const bool* exists,
+__device__ __forceinline__ void add_unit(float (*acc)[4], uint32_t stage, uint32_t values, const float* factors, uint32_t columns, const bool* exists,
                                          uint32_t lane) {
     const uint32_t g = lane >> 2;
     // ldmatrix: lanes 8i .. 8i + 7 give the rows of matrix i: rows 0-7 and 8-15 of the block, then of the next one
@@ -89,6 +105,7 @@ __device__ __forceinline__ void add_unit(float (*acc)[4], uint32_t stage, uint32
     const uint32_t row = stage + m * 64, turn = (m >> 1) & 3;
     const uint32_t at = stage + kUnitBytes + (g & 3) * 16 + (g >> 2) * 4;
     const uint32_t upper = lds32(at), lower = lds32(at + 8);    // four scale bytes of rows g and g + 8
+    float sum[NT][4] = {};
 #pragma unroll
     for (int pair = 0; pair < 2; ++pair) {
         uint32_t w[4];
@@ -101,29 +118,40 @@ __device__ __forceinline__ void add_unit(float (*acc)[4], uint32_t stage, uint32
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 uint4 x = make_uint4(0, 0, 0, 0);
-                if (exists[nt]) x = lds128(columns + (2 * pair + b) * block_bytes + nt * 8 * 64);
+                if (exists[nt]) x = lds128(values + (2 * pair + b) * columns * 64 + nt * 8 * 64);
                 float c[4] = {0.f, 0.f, 0.f, 0.f};
                 mma_f16(c, top.x, bottom.x, top.y, bottom.y, x.x, x.y);
                 mma_f16(c, top.z, bottom.z, top.w, bottom.w, x.z, x.w);
-                acc[nt][0] = fmaf(s0, c[0], acc[nt][0]);
-                acc[nt][1] = fmaf(s0, c[1], acc[nt][1]);
-                acc[nt][2] = fmaf(s1, c[2], acc[nt][2]);
-                acc[nt][3] = fmaf(s1, c[3], acc[nt][3]);
+                sum[nt][0] = fmaf(s0, c[0], sum[nt][0]);
+                sum[nt][1] = fmaf(s0, c[1], sum[nt][1]);
+                sum[nt][2] = fmaf(s1, c[2], sum[nt][2]);
+                sum[nt][3] = fmaf(s1, c[3], sum[nt][3]);
             }
         }
     }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const float f0 = factors[nt * 8], f1 = factors[nt * 8 + 1];
+        acc[nt][0] = fmaf(f0, sum[nt][0], acc[nt][0]);
+        acc[nt][1] = fmaf(f1, sum[nt][1], acc[nt][1]);
+        acc[nt][2] = fmaf(f0, sum[nt][2], acc[nt][2]);
+        acc[nt][3] = fmaf(f1, sum[nt][3], acc[nt][3]);
+    }
 }
 
-// The sums of this warp, scaled back, to shared memory: sums[row of the strip][column].
+// The sums of this warp to shared memory: sums[row of the strip][column].
 template <int NT>
-__device__ __forceinline__ void put_sums(float* sums, const float (*acc)[4], const float* inverse, uint32_t lane) {
+__device__ __forceinline__ void put_sums(float* sums, const float (*acc)[4], uint32_t lane) {
     const uint32_t g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        const float2 f = *reinterpret_cast<const float2*>(inverse + nt * 8 + 2 * t);
-        *reinterpret_cast<float2*>(sums + g * few_sum_row(NT) + nt * 8 + 2 * t) = make_float2(acc[nt][0] * f.x, acc[nt][1] * f.y);
-        *reinterpret_cast<float2*>(sums + (g + 8) * few_sum_row(NT) + nt * 8 + 2 * t) = make_float2(acc[nt][2] * f.x, acc[nt][3] * f.y);
+        *reinterpret_cast<float2*>(sums + g * few_sum_row(NT) + nt * 8 + 2 * t) = make_float2(acc[nt][0], acc[nt][1]);
+        *reinterpret_cast<float2*>(sums + (g + 8) * few_sum_row(NT) + nt * 8 + 2 * t) = make_float2(acc[nt][2], acc[nt][3]);
     }
+}
+// A barrier of one team's warps.
+__device__ __forceinline__ void team_sync(uint32_t team, uint32_t threads) {
+    asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(threads) : "memory");
 }
 
 // Row of the matrix (within the row tile) that row m of strip j is.
@@ -152,49 +180,42 @@ __device__ __forceinline__ uint4 pack_half8(const float* x) {
                       MicroType<ENEC_FP16>::pack(x[6], x[7]));
 }
 
-// Lays this warp's share of the columns out for add_unit: units warp, warp + kFewWarps, ... below `units`, each 128 values from
-// column `from` + 128 u on; values behind `cols` are zeros. Of every block of 32 values column after column, 64 bytes each, so a
-// block is 64 * columns bytes; row_of(i) is where the i-th column's values come from. Each is scaled by a power of two of the
-// warp's own, whose inverse goes to inverse[i]: no other warp reads these units, and sums are scaled back before they are joined.
+// Lays columns out for add_unit, by all warps of the CTA; barriers in front and behind are the caller's. Column i's values are
+// those of row_of(i) from `from` on, zeros behind `cols`. Of every 32 values column after column, 64 bytes each; half a warp takes 128
+// values of a column, and their factor's inverse goes to inverse[unit * pitch + column].
 template <int DT, class RowOf>
-__device__ __forceinline__ void stage_share(RowOf row_of, uint32_t columns, uint32_t units, uint32_t from, uint32_t cols, uint32_t dst,
-                                            float* inverse, uint32_t warp, uint32_t lane) {
+__device__ __forceinline__ void stage_columns(RowOf row_of, uint32_t columns, uint32_t units, uint32_t from, uint32_t cols, uint32_t dst,
+                                              float* inverse, uint32_t pitch) {
     constexpr int kElem = DT == ENEC_FP32 ? 4 : 2;
-    const uint32_t group = lane & 15;   // of eight values in a unit; half a warp takes a row
-    for (uint32_t first = 0; first < columns; first += 2) {
-        const uint32_t i = first + (lane >> 4);
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = lane & 15;
+    const uint32_t pairs = (columns + 1) / 2, tasks = pairs * units;
+#pragma unroll 2
+    for (uint32_t task = warp; task < tasks; task += kFewWarps) {
+        const uint32_t u = task / pairs, i = task % pairs * 2 + (lane >> 4);
         const bool mine = i < columns;
-        const uint8_t* row = mine ? row_of(i) : nullptr;
-        auto load = [&](uint32_t u, float* x) {
-            uint32_t w[2 * kElem];
-            const uint32_t col = from + u * kUnitCols + 8 * group;
-            load_eight<DT>(row + uint64_t(col) * kElem, mine && col < cols ? int(min(cols - col, 8u)) : 0, w);
-            as_floats<DT>(w, x);
-        };
+        const uint32_t col = from + u * kUnitCols + 8 * group;
+        uint32_t w[2 * kElem];
+        load_eight<DT>(mine ? row_of(i) + uint64_t(col) * kElem : nullptr, mine && col < cols ? int(min(cols - col, 8u)) : 0, w);
+        float x[8];
+        as_floats<DT>(w, x);
         uint32_t top = 0;
         if constexpr (DT != ENEC_FP16) {
-#pragma unroll 4
-            for (uint32_t u = warp; u < units; u += kFewWarps) {
-                float x[8];
-                load(u, x);
-                top = larger_finite(top, x);
-            }
+            top = larger_finite(0, x);
 #pragma unroll
             for (int d = 1; d < 16; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
         }
-        const float factor = DT == ENEC_FP16 ? 1.f : column_factor(top);
-        if (mine && group == 0) inverse[i] = DT == ENEC_FP16 ? 1.f : column_inverse(top);
-#pragma unroll 4
-        for (uint32_t u = warp; u < units; u += kFewWarps) {
-            float x[8];
-            load(u, x);
-            if (!mine) continue;
+        if (!mine) continue;
+        if (group == 0) inverse[u * pitch + i] = DT == ENEC_FP16 ? 1.f : column_inverse(top);
+        const uint32_t at = dst + (u * 4 + (group >> 2)) * columns * 64 + i * 64 + (group & 3) * 16;
+        if constexpr (DT == ENEC_FP16) {
+            sts128(at, make_uint4(w[0], w[1], w[2], w[3]));
+        } else {
+            const float factor = column_factor(top);
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] *= factor;
-            sts128(dst + (u * 4 + (group >> 2)) * columns * 64 + i * 64 + (group & 3) * 16, pack_half8(x));
+            sts128(at, pack_half8(x));
         }
     }
-    __syncwarp();
 }
 
 #endif  // __CUDACC__

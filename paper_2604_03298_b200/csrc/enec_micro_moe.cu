@@ -25,9 +25,8 @@ constexpr uint32_t kMoeCluster = 8;
 constexpr uint32_t kMoeMostTokens = 64;
 constexpr uint32_t kMoeMostExperts = 512;
 constexpr uint32_t kMoeMostTop = 16;
+constexpr uint32_t kMoeMostShared = kFewMostShared - 1024;   // the kernels have a little static shared memory too
 constexpr uint32_t kMoeMostLogits = 24576;   // tokens x experts: two such arrays of fp32 in shared memory
-constexpr int kStages1 = 3;                  // of a ring for two matrices; with two CTAs on an SM 70 KB in flight
-constexpr int kStages2 = 6;
 
 struct MoeJob {
     const uint8_t* x;
@@ -42,6 +41,7 @@ struct MoeJob {
     uint32_t tokens, hidden, inter, experts, top, renormalize;
     uint32_t strips_in, strips_out;
     uint32_t group;                  // pairs of a group, in this launch
+    uint32_t team;                   // warps of a team, in this launch
     uint32_t ld_h;
     uint32_t* pair_expert;
     float* pair_weight;
@@ -230,15 +230,6 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
     __syncthreads();
 }
 
-template <int NT>
-__host__ __device__ constexpr uint32_t moe_fixed1() {
-    return few_sum_bytes(NT, 2) + kFewWarps * 8 * NT * 4 + kFewWarps * kStages1 * few_stage_bytes(2);
-}
-template <int NT>
-__host__ __device__ constexpr uint32_t moe_fixed2() {
-    return few_sum_bytes(NT, 1) + kFewWarps * 8 * NT * 4 + kFewWarps * kStages2 * few_stage_bytes(1);
-}
-
 // The items of a CTA: [begin, end) of groups x strips, the strips of a group one after another.
 struct Share {
     uint32_t begin, end;
@@ -247,190 +238,169 @@ __device__ __forceinline__ Share share_of(uint64_t items) {
     return {uint32_t(items * blockIdx.x / gridDim.x), uint32_t(items * (blockIdx.x + 1) / gridDim.x)};
 }
 
-template <int DT, int NT>
-__global__ void __launch_bounds__(kFewThreads, 2) enec_moe_in_kernel(const __grid_constant__ MoeJob job) {
-    extern __shared__ __align__(128) uint8_t smem[];
+// A team's walk over its CTA's items: of every group's the team's own, every teams-th one.
+struct Walk {
+    uint32_t item, end, stop;        // the next item; where the CTA's items of its group end, and all of them
+    uint32_t strips, team, teams;
+    __device__ __forceinline__ void enter(uint32_t begin) {   // the group of item `begin`
+        const uint32_t group_end = (begin / strips + 1) * strips;
+        end = min(group_end, stop);
+        item = begin + team;
+    }
+    __device__ __forceinline__ void settle() {                // on to the next group that has an item for the team
+        while (item >= end && end < stop) enter(end);
+    }
+    __device__ __forceinline__ bool more() const { return item < end; }
+};
+
+// What both kernels do: the strips of `mats` matrices (gate and up, or down) of the CTA's groups times the groups' staged columns. `rows_of`
+// gives the values of a column, `finish` takes an item's sums (of the team's warps) between two barriers of the team.
+template <int DT, int NT, int MATS, class RowOf, class Finish>
+__device__ __forceinline__ void expert_products(const Routing& r, uint32_t group, uint32_t team_warps, const uint8_t* m0, const uint8_t* m1, const MicroShape& s,
+                                                uint32_t strips, uint8_t* smem, RowOf row_of, Finish finish) {
+    constexpr uint32_t kStages = few_stages(MATS), kSums = few_sum_words(NT, MATS);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const uint32_t pairs = job.tokens * job.top, tables = routing_bytes(pairs, job.experts);
-    const Routing r = routing_at(smem, pairs, job.experts);
-    float* sums = reinterpret_cast<float*>(smem + tables);
-    float* inverse = reinterpret_cast<float*>(smem + tables + few_sum_bytes(NT, 2)) + warp * 8 * NT;
-    const uint32_t ring = smem_u32(smem) + tables + few_sum_bytes(NT, 2) + kFewWarps * 8 * NT * 4 + warp * kStages1 * few_stage_bytes(2);
-    const uint32_t staged = smem_u32(smem) + tables + moe_fixed1<NT>();
-    pdl_wait();
-    pdl_launch_dependents();
-    route<DT>(job, r, sums);
-    build_lists(r, job.group);
-    if (blockIdx.x == 0) {
-        for (uint32_t p = threadIdx.x; p < pairs; p += kFewThreads) job.pair_expert[p] = r.expert[p], job.pair_weight[p] = r.weight[p];
-        for (uint32_t i = threadIdx.x; i < job.strips_out; i += kFewThreads) job.tickets[i] = 0;
-    }
-    const bool good = micro_header_ok(job.gate, job.s_in) && micro_header_ok(job.up, job.s_in);
-    if (!good) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
-        return;
-    }
-    const uint32_t units = (job.hidden + kUnitCols - 1) / kUnitCols;
-    const Share mine = share_of(uint64_t(r.group_first[job.experts]) * job.strips_in);
-    uint32_t ask_item = mine.begin, ask_u = warp, slot = 0, ask_group = 0xFFFFFFFFu;
+    const uint32_t units = (s.cols + kUnitCols - 1) / kUnitCols;
+    const uint32_t team = warp / team_warps, in_team = warp % team_warps, teams = kFewWarps / team_warps;
+    float* sums = reinterpret_cast<float*>(smem + few_ring_bytes(MATS)) + team * team_warps * kSums;
+    float* inverse = reinterpret_cast<float*>(smem + few_fixed_bytes(NT, MATS));
+    const uint32_t ring = smem_u32(smem) + warp * kStages * few_stage_bytes(MATS);
+    const uint32_t staged = smem_u32(inverse + units * 8 * NT);
+    const Share mine = share_of(uint64_t(r.group_first[r.experts]) * strips);
+    if (mine.begin == mine.end) return;
+    Walk asked{0, 0, mine.end, strips, team, teams};
+    asked.enter(mine.begin);
+    asked.settle();
+    uint32_t ask_u = in_team, slot = 0, ask_group = 0xFFFFFFFFu;
     uint64_t ask_matrix = 0;
     auto ask = [&]() {
-        if (ask_item < mine.end && ask_u < units) {
-            const uint32_t index = ask_item / job.strips_in, strip = ask_item % job.strips_in;
+        if (asked.more() && ask_u < units) {
+            const uint32_t index = asked.item / strips, strip = asked.item % strips;
             if (index != ask_group) {
                 ask_group = index;
-                ask_matrix = uint64_t(group_of(r, index, job.group).expert) * job.s_in.row_tiles;
+                ask_matrix = uint64_t(group_of(r, index, group).expert) * s.row_tiles;
             }
-            const uint64_t at = kMicroHeaderBytes + (ask_matrix + (strip >> 3)) * job.s_in.col_tiles * kMicroRecordBytes;
-            const uint32_t stage = ring + slot * few_stage_bytes(2);
-            ask_unit(job.gate + at, strip & 7, ask_u, stage, lane);
-            ask_unit(job.up + at, strip & 7, ask_u, stage + few_stage_bytes(1), lane);
-            ask_u += kFewWarps;
-            if (ask_u >= units) ask_u = warp, ++ask_item;
+            const uint64_t at = kMicroHeaderBytes + (ask_matrix + (strip >> 3)) * s.col_tiles * kMicroRecordBytes;
+            const uint32_t stage = ring + slot * few_stage_bytes(MATS);
+            ask_unit(m0 + at, strip & 7, ask_u, stage, lane);
+            if (MATS == 2) ask_unit(m1 + at, strip & 7, ask_u, stage + few_stage_bytes(1), lane);
+            ask_u += team_warps;
+            if (ask_u >= units) {
+                ask_u = in_team;
+                asked.item += teams;
+                asked.settle();
+            }
         }
         cp_async_commit();
-        slot = slot + 1 == kStages1 ? 0 : slot + 1;
+        slot = slot + 1 == kStages ? 0 : slot + 1;
     };
 #pragma unroll
-    for (int i = 0; i < kStages1 - 1; ++i) ask();
-    if (lane < 8 * NT) inverse[lane] = 0.f;
-    __syncwarp();
-    Group now = {};
-    uint32_t staged_group = 0xFFFFFFFFu, from = 0, set = 0, block_bytes = 0;
-    bool exists[NT] = {};
-    const uint32_t columns = staged + g * 64 + t * 16;
-    for (uint32_t item = mine.begin; item < mine.end; ++item) {
-        const uint32_t index = item / job.strips_in, strip = item % job.strips_in;
-        if (index != staged_group) {
-            staged_group = index;
-            now = group_of(r, index, job.group);
-            block_bytes = now.n * 64;
-            __syncwarp();   // this warp's lanes have read the columns of the group before
-            stage_share<DT>([&](uint32_t i) { return job.x + uint64_t(r.list[now.first + i] / job.top) * job.ld_x * 2; }, now.n, units, 0, job.hidden,
-                            staged, inverse, warp, lane);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) exists[nt] = nt * 8 + g < now.n;
-        }
-        float a[NT][4] = {}, b[NT][4] = {};
-        for (uint32_t u = warp; u < units; u += kFewWarps) {
-            cp_async_wait<kStages1 - 2>();
-            __syncwarp();
-            ask();
-            const uint32_t stage = ring + from * few_stage_bytes(2);
-            add_unit<NT>(a, stage, columns + u * 4 * block_bytes, block_bytes, exists, lane);
-            add_unit<NT>(b, stage + few_stage_bytes(1), columns + u * 4 * block_bytes, block_bytes, exists, lane);
-            from = from + 1 == kStages1 ? 0 : from + 1;
-        }
-        float* here = sums + set * (few_sum_bytes(NT, 2) / 8);
-        put_sums<NT>(here + warp * 16 * few_sum_row(NT), a, inverse, lane);
-        put_sums<NT>(here + (kFewWarps + warp) * 16 * few_sum_row(NT), b, inverse, lane);
+    for (uint32_t i = 0; i < kStages - 1; ++i) ask();
+    const uint32_t values = staged + g * 64 + t * 16;
+    uint32_t from = 0;
+    Walk walk{0, 0, mine.end, strips, team, teams};
+    for (uint32_t begin = mine.begin; begin < mine.end; begin = walk.end) {
+        walk.enter(begin);
+        const Group now = group_of(r, begin / strips, group);
+        __syncthreads();   // the columns of the group before have been used
+        stage_columns<DT>([&](uint32_t i) { return row_of(r.list[now.first + i]); }, now.n, units, 0, s.cols, staged, inverse, 8 * NT);
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < 16 * now.n; i += kFewThreads) {
-            const uint32_t m = i & 15, column = i >> 4;
-            const uint32_t row = (strip >> 3) * kMicroRows + strip_row(strip & 7, m);
-            float u = 0.f, v = 0.f;
+        bool exists[NT];
 #pragma unroll
-            for (uint32_t k = 0; k < kFewWarps; ++k) {
-                u += here[(k * 16 + m) * few_sum_row(NT) + column];
-                v += here[((kFewWarps + k) * 16 + m) * few_sum_row(NT) + column];
+        for (int nt = 0; nt < NT; ++nt) exists[nt] = nt * 8 + g < now.n;
+        for (; walk.more(); walk.item += teams) {
+            float acc[MATS][NT][4] = {};
+            for (uint32_t u = in_team; u < units; u += team_warps) {
+                cp_async_wait<kStages - 2>();
+                __syncwarp();
+                ask();   // into the slot that the unit before was read from, by all lanes
+#pragma unroll
+                for (int i = 0; i < MATS; ++i)
+                    add_unit<NT>(acc[i], ring + from * few_stage_bytes(MATS) + i * few_stage_bytes(1), values + u * 4 * now.n * 64,
+                                 inverse + u * 8 * NT + 2 * t, now.n, exists, lane);
+                from = from + 1 == kStages ? 0 : from + 1;
             }
-            if (row < job.inter) job.h[uint64_t(r.list[now.first + column]) * job.ld_h + row] = u / (1.f + expf(-u)) * v;
+#pragma unroll
+            for (int i = 0; i < MATS; ++i) put_sums<NT>(sums + in_team * kSums + i * few_sum_words(NT, 1), acc[i], lane);
+            team_sync(team, team_warps * 32);
+            finish(now, walk.item % strips, sums, in_team * 32 + lane, team);
+            team_sync(team, team_warps * 32);   // the sums have been read before they are written again
         }
-        set ^= 1;
     }
     cp_async_wait<0>();
 }
 
 template <int DT, int NT>
-__global__ void __launch_bounds__(kFewThreads, 2) enec_moe_out_kernel(const __grid_constant__ MoeJob job) {
+__global__ void __launch_bounds__(kFewThreads, 1) enec_moe_in_kernel(const __grid_constant__ MoeJob job) {
     extern __shared__ __align__(128) uint8_t smem[];
-    using T = typename MicroType<DT>::T;
-    __shared__ uint32_t last;
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const uint32_t pairs = job.tokens * job.top, tables = routing_bytes(pairs, job.experts);
     const Routing r = routing_at(smem, pairs, job.experts);
-    float* sums = reinterpret_cast<float*>(smem + tables);
-    float* inverse = reinterpret_cast<float*>(smem + tables + few_sum_bytes(NT, 1)) + warp * 8 * NT;
-    const uint32_t ring = smem_u32(smem) + tables + few_sum_bytes(NT, 1) + kFewWarps * 8 * NT * 4 + warp * kStages2 * few_stage_bytes(1);
-    const uint32_t staged = smem_u32(smem) + tables + moe_fixed2<NT>();
+    pdl_wait();
+    pdl_launch_dependents();
+    route<DT>(job, r, reinterpret_cast<float*>(smem + tables));
+    build_lists(r, job.group);
+    if (blockIdx.x == 0) {
+        for (uint32_t p = threadIdx.x; p < pairs; p += kFewThreads) job.pair_expert[p] = r.expert[p], job.pair_weight[p] = r.weight[p];
+        for (uint32_t i = threadIdx.x; i < job.strips_out; i += kFewThreads) job.tickets[i] = 0;
+    }
+    if (!micro_header_ok(job.gate, job.s_in) || !micro_header_ok(job.up, job.s_in)) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
+        return;
+    }
+    expert_products<DT, NT, 2>(
+        r, job.group, job.team, job.gate, job.up, job.s_in, job.strips_in, smem + tables,
+        [&](uint32_t pair) { return job.x + uint64_t(pair / job.top) * job.ld_x * 2; },
+        [&](const Group& now, uint32_t strip, const float* sums, uint32_t thread, uint32_t) {
+            for (uint32_t i = thread; i < 16 * now.n; i += job.team * 32) {
+                const uint32_t m = i & 15, column = i >> 4;
+                const uint32_t row = (strip >> 3) * kMicroRows + strip_row(strip & 7, m);
+                float u = 0.f, v = 0.f;
+                for (uint32_t k = 0; k < job.team; ++k) {
+                    const float* theirs = sums + k * few_sum_words(NT, 2) + m * few_sum_row(NT) + column;
+                    u += theirs[0];
+                    v += theirs[few_sum_words(NT, 1)];
+                }
+                if (row < job.inter) job.h[uint64_t(r.list[now.first + column]) * job.ld_h + row] = u / (1.f + expf(-u)) * v;
+            }
+        });
+}
+
+template <int DT, int NT>
+__global__ void __launch_bounds__(kFewThreads, 1) enec_moe_out_kernel(const __grid_constant__ MoeJob job) {
+    extern __shared__ __align__(128) uint8_t smem[];
+    using T = typename MicroType<DT>::T;
+    __shared__ uint32_t last[kFewWarps / 4];   // of each team
+    const uint32_t pairs = job.tokens * job.top, tables = routing_bytes(pairs, job.experts);
+    const Routing r = routing_at(smem, pairs, job.experts);
     pdl_wait();
     pdl_launch_dependents();
     for (uint32_t p = threadIdx.x; p < pairs; p += kFewThreads) r.expert[p] = uint16_t(job.pair_expert[p]), r.weight[p] = job.pair_weight[p];
-    const bool good = micro_header_ok(job.gate, job.s_in) && micro_header_ok(job.up, job.s_in) && micro_header_ok(job.down, job.s_out);
-    if (!good) {
+    if (!micro_header_ok(job.gate, job.s_in) || !micro_header_ok(job.up, job.s_in) || !micro_header_ok(job.down, job.s_out)) {
         if (blockIdx.x == 0 && threadIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
         return;
     }
     __syncthreads();
     build_lists(r, job.group);
-    const uint32_t units = (job.inter + kUnitCols - 1) / kUnitCols, groups = r.group_first[job.experts];
-    const Share mine = share_of(uint64_t(groups) * job.strips_out);
-    uint32_t ask_item = mine.begin, ask_u = warp, slot = 0, ask_group = 0xFFFFFFFFu;
-    uint64_t ask_matrix = 0;
-    auto ask = [&]() {
-        if (ask_item < mine.end && ask_u < units) {
-            const uint32_t index = ask_item / job.strips_out, strip = ask_item % job.strips_out;
-            if (index != ask_group) {
-                ask_group = index;
-                ask_matrix = uint64_t(group_of(r, index, job.group).expert) * job.s_out.row_tiles;
+    const uint32_t groups = r.group_first[job.experts];
+    expert_products<ENEC_FP32, NT, 1>(
+        r, job.group, job.team, job.down, nullptr, job.s_out, job.strips_out, smem + tables,
+        [&](uint32_t pair) { return reinterpret_cast<const uint8_t*>(job.h + uint64_t(pair) * job.ld_h); },
+        [&](const Group& now, uint32_t strip, const float* sums, uint32_t thread, uint32_t team) {
+            for (uint32_t i = thread; i < 16 * now.n; i += job.team * 32) {
+                const uint32_t m = i & 15, column = i >> 4, pair = r.list[now.first + column];
+                const uint32_t row = (strip >> 3) * kMicroRows + strip_row(strip & 7, m);
+                float v = 0.f;
+                for (uint32_t k = 0; k < job.team; ++k) v += sums[k * few_sum_words(NT, 1) + m * few_sum_row(NT) + column];
+                if (row < job.hidden) __stcg(job.partial + uint64_t(pair) * job.hidden + row, v * r.weight[pair]);
             }
-            const uint64_t at = kMicroHeaderBytes + (ask_matrix + (strip >> 3)) * job.s_out.col_tiles * kMicroRecordBytes;
-            ask_unit(job.down + at, strip & 7, ask_u, ring + slot * few_stage_bytes(1), lane);
-            ask_u += kFewWarps;
-            if (ask_u >= units) ask_u = warp, ++ask_item;
-        }
-        cp_async_commit();
-        slot = slot + 1 == kStages2 ? 0 : slot + 1;
-    };
-#pragma unroll
-    for (int i = 0; i < kStages2 - 1; ++i) ask();
-    if (lane < 8 * NT) inverse[lane] = 0.f;
-    __syncwarp();
-    Group now = {};
-    uint32_t staged_group = 0xFFFFFFFFu, from = 0, set = 0, block_bytes = 0;
-    bool exists[NT] = {};
-    const uint32_t columns = staged + g * 64 + t * 16;
-    for (uint32_t item = mine.begin; item < mine.end; ++item) {
-        const uint32_t index = item / job.strips_out, strip = item % job.strips_out;
-        if (index != staged_group) {
-            staged_group = index;
-            now = group_of(r, index, job.group);
-            block_bytes = now.n * 64;
-            __syncwarp();
-            stage_share<ENEC_FP32>(
-                [&](uint32_t i) { return reinterpret_cast<const uint8_t*>(job.h + uint64_t(r.list[now.first + i]) * job.ld_h); }, now.n, units, 0,
-                job.inter, staged, inverse, warp, lane);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) exists[nt] = nt * 8 + g < now.n;
-        }
-        float a[NT][4] = {};
-        for (uint32_t u = warp; u < units; u += kFewWarps) {
-            cp_async_wait<kStages2 - 2>();
-            __syncwarp();
-            ask();
-            add_unit<NT>(a, ring + from * few_stage_bytes(1), columns + u * 4 * block_bytes, block_bytes, exists, lane);
-            from = from + 1 == kStages2 ? 0 : from + 1;
-        }
-        float* here = sums + set * (few_sum_bytes(NT, 1) / 8);
-        put_sums<NT>(here + warp * 16 * few_sum_row(NT), a, inverse, lane);
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < 16 * now.n; i += kFewThreads) {
-            const uint32_t m = i & 15, column = i >> 4, pair = r.list[now.first + column];
-            const uint32_t row = (strip >> 3) * kMicroRows + strip_row(strip & 7, m);
-            float v = 0.f;
-#pragma unroll
-            for (uint32_t k = 0; k < kFewWarps; ++k) v += here[(k * 16 + m) * few_sum_row(NT) + column];
-            if (row < job.hidden) __stcg(job.partial + uint64_t(pair) * job.hidden + row, v * r.weight[pair]);
-        }
-        set ^= 1;
-        // every thread's sums are visible to all before the ticket counts the item
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) last = atomicAdd(job.tickets + strip, 1u) == groups - 1;
-        __syncthreads();
-        if (last) {
+            // every thread's values are visible to all before the ticket counts the item
             __threadfence();
-            for (uint32_t i = threadIdx.x; i < 16 * job.tokens; i += kFewThreads) {
+            team_sync(team, job.team * 32);
+            if (thread == 0) last[team] = atomicAdd(job.tickets + strip, 1u) == groups - 1;
+            team_sync(team, job.team * 32);
+            if (!last[team]) return;
+            __threadfence();
+            for (uint32_t i = thread; i < 16 * job.tokens; i += job.team * 32) {
                 const uint32_t m = i & 15, token = i >> 4;
                 const uint32_t row = (strip >> 3) * kMicroRows + strip_row(strip & 7, m);
                 if (row >= job.hidden) continue;
@@ -438,9 +408,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) enec_moe_out_kernel(const __gr
                 for (uint32_t j = 0; j < job.top; ++j) v += __ldcg(job.partial + uint64_t(token * job.top + j) * job.hidden + row);
                 reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
             }
-        }
-    }
-    cp_async_wait<0>();
+        });
 }
 
 uint32_t strips_of(const MicroShape& s) {
@@ -448,16 +416,13 @@ uint32_t strips_of(const MicroShape& s) {
     return (s.row_tiles - 1) * 8 + (last >= 32 ? 8 : (last + 3) / 4);
 }
 
-// Pairs per group, and with them the shared memory: as many as there may be, on half an SM's memory if eight (or all) fit there.
-bool choose_group(uint32_t fixed, uint32_t units, uint32_t most, uint32_t least_bytes, uint32_t& group, uint32_t& bytes) {
-    const uint64_t per = uint64_t(units) * kUnitCols * 2;
-    for (uint32_t cap : {kFewMostShared / 2 - 1024, kFewMostShared - 1024}) {
-        const uint64_t fit = cap > fixed ? (cap - fixed) / per : 0;
-        if (cap < least_bytes || fit < (cap > kFewMostShared / 2 ? 1 : most < 8 ? most : 8)) continue;
-        group = fit < most ? uint32_t(fit) : most;
-        const uint64_t need = fixed + group * per;
+// Pairs per group, and with them the shared memory: as many as there may be.
+bool choose_group(uint32_t fixed, uint32_t units, int nt, uint32_t most, uint32_t least_bytes, uint32_t& group, uint32_t& bytes) {
+    for (group = most; group > 0; --group) {
+        const uint64_t need = fixed + uint64_t(units) * few_unit_bytes(nt, group);
+        if (need > kMoeMostShared) continue;
         bytes = need > least_bytes ? uint32_t(need) : least_bytes;
-        return true;
+        return bytes <= kMoeMostShared;
     }
     return false;
 }
@@ -495,16 +460,19 @@ enec_status launch_moe(MoeJob job, const MicroDevice& dev, cudaStream_t stream) 
     const uint32_t most = 8 * NT < job.tokens ? 8 * NT : job.tokens;   // an expert has at most one pair of a token
     uint32_t bytes = 0, clusters = 0;
     static std::atomic<uint64_t> allowed_in{0}, allowed_out{0};
-    if (!choose_group(tables + moe_fixed1<NT>(), (job.hidden + kUnitCols - 1) / kUnitCols, most, tables + 8 * job.tokens * job.experts, job.group,
-                      bytes))
-        return ENEC_ERR_TOO_LARGE;
+    const uint32_t units_in = (job.hidden + kUnitCols - 1) / kUnitCols, units_out = (job.inter + kUnitCols - 1) / kUnitCols;
     MoeJob second = job;
     uint32_t bytes2 = 0;
-    if (!choose_group(tables + moe_fixed2<NT>(), (job.inter + kUnitCols - 1) / kUnitCols, most, 0, second.group, bytes2)) return ENEC_ERR_TOO_LARGE;
-    if (!allow_shared(allowed_in, dev, enec_moe_in_kernel<DT, NT>, kFewMostShared - 1024) ||
-        !allow_shared(allowed_out, dev, enec_moe_out_kernel<DT, NT>, kFewMostShared - 1024) ||
+    if (!choose_group(tables + few_fixed_bytes(NT, 2), units_in, NT, most, tables + 8 * job.tokens * job.experts, job.group, bytes) ||
+        !choose_group(tables + few_fixed_bytes(NT, 1), units_out, NT, most, 0, second.group, bytes2))
+        return ENEC_ERR_TOO_LARGE;
+    if (!allow_shared(allowed_in, dev, enec_moe_in_kernel<DT, NT>, kMoeMostShared) ||
+        !allow_shared(allowed_out, dev, enec_moe_out_kernel<DT, NT>, kMoeMostShared) ||
         !resident_clusters(enec_moe_in_kernel<DT, NT>, dev, bytes, clusters))
         return ENEC_ERR_CUDA;
+    const uint64_t used = pairs < job.experts ? pairs : job.experts;   // experts with work, at most
+    job.team = few_team(used * job.strips_in, units_in, clusters * kMoeCluster);
+    second.team = few_team(used * job.strips_out, units_out, uint32_t(dev.sms));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(clusters * kMoeCluster);
     cfg.blockDim = dim3(kFewThreads);
@@ -521,8 +489,7 @@ enec_status launch_moe(MoeJob job, const MicroDevice& dev, cudaStream_t stream) 
     cudaError_t err = cudaLaunchKernelEx(&cfg, enec_moe_in_kernel<DT, NT>, job);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     if (err != cudaSuccess) return ENEC_ERR_CUDA;
-    const uint32_t grid = uint32_t(dev.sms) * (bytes2 <= kFewMostShared / 2 - 1024 ? 2 : 1);
-    err = launch_pdl(enec_moe_out_kernel<DT, NT>, grid, kFewThreads, bytes2, stream, second);
+    err = launch_pdl(enec_moe_out_kernel<DT, NT>, uint32_t(dev.sms), kFewThreads, bytes2, stream, second);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return err == cudaSuccess ? ENEC_OK : ENEC_ERR_CUDA;
 }
@@ -592,7 +559,7 @@ extern "C" enec_status enec_moe_microscaled(const void* d_x, enec_dtype dt, size
     job.renormalize = renormalize != 0;
     job.strips_in = strips_of(job.s_in);
     job.strips_out = strips_of(job.s_out);
-    job.group = 0;
+    job.group = job.team = 0;
     job.ld_h = l.ld_h;
     job.pair_expert = reinterpret_cast<uint32_t*>(ws);
     job.pair_weight = reinterpret_cast<float*>(ws + l.weight);
