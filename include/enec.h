@@ -236,8 +236,10 @@ enec_status enec_dequantize_microscaled(const void* d_in, size_t in_size, enec_d
 
 /*
  * y = x W^T: x [tokens, cols] and y [tokens, rows] of type dt (bf16 or fp16), W a stream of one matrix of rows x cols. Sums are in fp32,
- * y is rounded once; neither x nor W is rounded on the way. From one token (bound by the weights' bytes) to thousands (tensor
- * cores). tokens == 0 or rows == 0 is valid and does nothing; cols == 0 gives zeros. x and y must not overlap.
+ * y is rounded once, W not at all. Up to 16 tokens, a value of x counts to 2^-22 of the largest of the 32 neighbours (columns 32c ..) that
+ * it stands among: beyond a bf16 value's last bit for all within 2^-14 of that largest one. With more tokens x is not rounded
+ * either. A token with an infinity or a NaN has infinities or NaN in all of its results. From one token (bound by the weights' bytes) to
+ * thousands (bound by the tensor cores). tokens == 0 or rows == 0 is valid and does nothing; cols == 0 gives zeros. x and y must not overlap.
  */
 enec_status enec_matmul_microscaled(const void* d_x, enec_dtype dt, size_t tokens, size_t ld_x, const void* d_w, size_t w_size,
                                     size_t rows, size_t cols, void* d_y, size_t ld_y, int* d_status, enec_stream_t stream);
@@ -256,10 +258,10 @@ enec_status enec_matmul_microscaled_both(const void* d_x, size_t x_size, size_t 
  *   l = x R^T, p = softmax(l); a token's experts are the top_k with the largest l (ties: the lower number; a NaN counts as the
  *   smallest); their weights are p, with `renormalize` divided by the chosen ones' sum;
  *   y = sum over the chosen experts of weight * (silu(x G^T) * (x U^T)) D^T, silu(a) = a / (1 + exp(-a)).
- * Sums are in fp32; the hidden values are rounded to fp16's 11 bits (scaled: no overflow) on their way into the last product, y once.
+ * Sums are in fp32 and y is rounded once; x and the hidden values in fp32 count to 2^-22 of the largest of their 32 neighbours.
  * tokens <= 64, experts <= 512, top_k <= min(16, experts), tokens * experts <= 24576, else ENEC_ERR_TOO_LARGE or, for top_k beyond
  * experts and for sizes of zero, ENEC_ERR_INVALID_ARG; ENEC_ERR_TOO_LARGE too where not one token's row of hidden or inter values fits
- * into an SM's shared memory (about 60000 values). tokens == 0 is valid and does nothing.
+ * into an SM's shared memory (about 12000 values). tokens == 0 is valid and does nothing.
  * d_workspace: enec_moe_microscaled_workspace bytes of device memory, 16-byte aligned, of any content; the call uses it from its
  * beginning to its end, so calls that may overlap on the GPU need one each.
  */

@@ -1,9 +1,9 @@
-// y = x W^T for few tokens, W a microscaled stream: one launch that reads every weight once (see enec_micro_few.cuh).
+// y = x W^T for few tokens, W a microscaled stream: one launch that reads every weight once (see enec_micro_pieces.cuh).
 //
-// A CTA's teams take strips of 16 rows, one after another. The activations stand in its shared memory, 2 bytes a value and token. Where
-// they would not fit, a cluster of CTAs shares the columns and the first of them adds the others' sums, in their order. No sum
-// depends on which team or CTA was faster.
-#include "enec_micro_few.cuh"
+// A CTA takes row tiles of W, one after another. Where there are fewer of them than SMs, or where the digits of whole rows of x would not
+// fit into shared memory, a cluster of CTAs shares the columns: each leaves its sums in its shared memory and adds up a part of the
+// tokens, in the order of the CTAs. No sum depends on which CTA was faster.
+#include "enec_micro_pieces.cuh"
 
 #include <cooperative_groups.h>
 
@@ -20,136 +20,126 @@ struct FewJob {
     uint8_t* y;
     uint64_t ld_y;
     uint32_t tokens;
-    uint32_t strips;      // that hold rows of the matrix
-    uint32_t share;       // units of 128 columns that a CTA of the cluster takes
+    uint32_t share;       // records of columns that a CTA of the cluster takes
     uint32_t cluster;
-    uint32_t team;        // warps
+    uint32_t stages;
     int* status;
 };
 
-template <int DT, int NT>
-__global__ void __launch_bounds__(kFewThreads, 1) enec_micro_few_kernel(const __grid_constant__ FewJob job) {
-    extern __shared__ __align__(128) uint8_t smem[];
+template <int DT>
+__global__ void __launch_bounds__(kPieceThreads, 1) enec_micro_few_kernel(const __grid_constant__ FewJob job) {
+    extern __shared__ uint8_t raw[];
+    __shared__ PieceShared sh;
     using T = typename MicroType<DT>::T;
-    constexpr uint32_t kStages = few_stages(1), kSums = few_sum_words(NT, 1);
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const MicroShape& s = job.s;
+    uint8_t* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = job.cluster > 1 ? blockIdx.x % job.cluster : 0;
-    const uint32_t all_units = (s.cols + kUnitCols - 1) / kUnitCols;
-    const uint32_t unit0 = min(rank * job.share, all_units), units = min(job.share, all_units - unit0);
-    const uint32_t per_cta = kFewWarps / job.team, team = warp / job.team, in_team = warp % job.team;
-    const uint32_t first = blockIdx.x / job.cluster * per_cta + team, step = gridDim.x / job.cluster * per_cta;
-    float* sums = reinterpret_cast<float*>(smem + few_ring_bytes(1)) + team * job.team * kSums;
-    float* inverse = reinterpret_cast<float*>(smem + few_fixed_bytes(NT, 1));
-    const uint32_t ring = smem_u32(smem) + warp * kStages * few_stage_bytes(1);
-    const uint32_t staged = smem_u32(inverse + job.share * 8 * NT);
-
+    const uint32_t first_tile = blockIdx.x / job.cluster, step = gridDim.x / job.cluster;
+    const uint32_t n_tasks = (job.s.row_tiles - first_tile + step - 1) / step;
+    const uint32_t first = min(rank * job.share, job.s.col_tiles), count = min(job.share, job.s.col_tiles - first);
+    const uint32_t columns = piece_columns(job.tokens), record_bytes = piece_record_bytes(job.tokens);
+    float* sums = reinterpret_cast<float*>(smem + job.stages * kMicroRecordBytes + job.share * record_bytes);   // two sets of [token][row]
+    piece_setup(sh, job.stages);
     pdl_wait();
     pdl_launch_dependents();
-    // what this warp asks for next: unit ask_u of strip ask_strip
-    uint32_t ask_strip = first, ask_u = in_team, slot = 0;
-    auto ask = [&]() {
-        if (ask_strip < job.strips && ask_u < units) {
-            ask_unit(job.w + kMicroHeaderBytes + uint64_t(ask_strip >> 3) * s.col_tiles * kMicroRecordBytes, ask_strip & 7, unit0 + ask_u,
-                     ring + slot * few_stage_bytes(1), lane);
-            ask_u += job.team;
-            if (ask_u >= units) ask_u = in_team, ask_strip += step;
-        }
-        cp_async_commit();
-        slot = slot + 1 == kStages ? 0 : slot + 1;
-    };
-#pragma unroll
-    for (uint32_t i = 0; i < kStages - 1; ++i) ask();
-    const bool good = micro_header_ok(job.w, s);
-    stage_columns<DT>([&](uint32_t i) { return job.x + uint64_t(i) * job.ld_x * sizeof(T); }, job.tokens, units, unit0 * kUnitCols, s.cols, staged,
-                      inverse, 8 * NT);
-    __syncthreads();
-    if (!good && blockIdx.x == 0 && threadIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
-
-    const uint32_t values = staged + g * 64 + t * 16;
-    bool exists[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) exists[nt] = nt * 8 + g < job.tokens;
-    uint32_t from = 0;
-    // clusters meet at every strip, so all their teams go round equally often
-    for (uint32_t strip = first; job.cluster > 1 ? strip - team < job.strips : strip < job.strips; strip += step) {
-        float acc[NT][4] = {};
-        for (uint32_t u = in_team; strip < job.strips && u < units; u += job.team) {
-            cp_async_wait<kStages - 2>();
-            __syncwarp();
-            ask();   // into the slot that the unit before was read from, by all lanes
-            add_unit<NT>(acc, ring + from * few_stage_bytes(1), values + u * 4 * job.tokens * 64, inverse + u * 8 * NT + 2 * t, job.tokens, exists, lane);
-            from = from + 1 == kStages ? 0 : from + 1;
-        }
-        put_sums<NT>(sums + in_team * kSums, acc, lane);
-        if (job.cluster > 1) cooperative_groups::this_cluster().sync();
-        else team_sync(team, job.team * 32);
-        if (rank == 0 && strip < job.strips) {
-            for (uint32_t i = in_team * 32 + lane; i < 16 * job.tokens; i += job.team * 32) {
-                const uint32_t m = i & 15, token = i >> 4;
-                const uint32_t row = (strip >> 3) * kMicroRows + strip_row(strip & 7, m);
-                float v = 0.f;
-                for (uint32_t r = 0; r < job.cluster; ++r) {
-                    const float* theirs = r ? cooperative_groups::this_cluster().map_shared_rank(sums, r) : sums;
-                    for (uint32_t k = 0; k < job.team; ++k) v += theirs[k * kSums + m * few_sum_row(NT) + token];
-                }
-                if (row < s.rows && good) reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
+    const bool good = micro_header_ok(job.w, job.s);
+    const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
+    piece_products(
+        sh, smem, job.stages, n_tasks, job.s.cols,
+        [&](uint32_t i) {
+            return PieceTask{job.w + kMicroHeaderBytes + uint64_t(first_tile + i * step) * job.s.col_tiles * kMicroRecordBytes, first, count, 0, 0};
+        },
+        [&](uint32_t, uint32_t at) {
+            for (uint32_t task = worker; task < count * job.tokens; task += kPieceWorkers) {
+                const uint32_t k = task / job.tokens, token = task % job.tokens;
+                const uint32_t col = (first + k) * kMicroCols + 8 * lane;
+                uint32_t w[4];
+                load_eight<DT>(job.x + (uint64_t(token) * job.ld_x + col) * 2, col < job.s.cols ? int(min(job.s.cols - col, 8u)) : 0, w);
+                float x[8];
+                as_floats<DT>(w, x);
+                put_digits(x, token, at + k * record_bytes, columns, lane);
             }
-        }
-        // the sums have been read before they are written again, and before a CTA ends
-        if (job.cluster > 1) cooperative_groups::this_cluster().sync();
-        else team_sync(team, job.team * 32);
+        },
+        [&](uint32_t) { return columns; },
+        [&](uint32_t i, uint32_t tmem, bool ok) {
+            const uint32_t row = (first_tile + i * step) * kMicroRows + row_in;
+            for (uint32_t token = worker >> 2; token < job.tokens; token += kPieceWorkers / 4) {
+                const float v = count ? take_sum(tmem, token) : 0.f;
+                if (job.cluster > 1) sums[((i & 1) * job.tokens + token) * kMicroRows + row_in] = v;
+                else if (good && ok && row < job.s.rows) reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
+            }
+        },
+        [&](uint32_t i) {
+            if (job.cluster == 1) {
+                __syncthreads();
+                return;
+            }
+            auto cluster = cooperative_groups::this_cluster();
+            cluster.sync();   // a set of sums is written again behind the next one of these, and has been read by then
+            const uint32_t r = threadIdx.x & 127, row = (first_tile + i * step) * kMicroRows + r;
+            if (threadIdx.x >= 512 || row >= job.s.rows || !good || sh.failed) return;
+            for (uint32_t token = (threadIdx.x >> 7) * job.cluster + rank; token < job.tokens; token += 4 * job.cluster) {
+                float v = 0.f;
+                for (uint32_t k = 0; k < job.cluster; ++k) v += cluster.map_shared_rank(sums, k)[((i & 1) * job.tokens + token) * kMicroRows + r];
+                reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
+            }
+        });
+    if (threadIdx.x == 0) {
+        if (sh.failed) report(job.status, ENEC_ERR_TIMEOUT);
+        else if (!good && blockIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
     }
-    cp_async_wait<0>();
+    if (job.cluster > 1) cooperative_groups::this_cluster().sync();   // no CTA ends while its sums are read
 }
 
-template <int DT, int NT>
+// Shared memory of a CTA that takes `share` records with four stages, or 0 where it does not fit.
+uint32_t few_bytes(uint32_t share, uint32_t tokens, uint32_t cluster, uint32_t& stages) {
+    const uint64_t others = 1024 + uint64_t(share) * piece_record_bytes(tokens) + (cluster > 1 ? tokens * kMicroRows * 8 : 0);
+    if (others + 4 * kMicroRecordBytes > kFewMostShared) return 0;
+    const uint64_t fit = (kFewMostShared - others) / kMicroRecordBytes;
+    stages = fit < kPieceMostStages ? uint32_t(fit) : kPieceMostStages;
+    return uint32_t(others + stages * kMicroRecordBytes);
+}
+
+template <int DT>
 enec_status launch(FewJob job, const MicroDevice& dev, cudaStream_t stream) {
-    const uint32_t all_units = (job.s.cols + kUnitCols - 1) / kUnitCols;
-    const uint32_t per_unit = few_unit_bytes(NT, job.tokens), fixed = few_fixed_bytes(NT, 1);
-    uint32_t cluster = 1;
-    while (cluster < 8 && fixed + uint64_t(all_units + cluster - 1) / cluster * per_unit > kFewMostShared) cluster *= 2;
-    job.cluster = cluster;
-    job.share = (all_units + cluster - 1) / cluster;
-    const uint32_t bytes = fixed + job.share * per_unit;
-    if (bytes > kFewMostShared) return ENEC_ERR_TOO_LARGE;
+    // the smallest cluster whose CTAs have room; a larger one as long as all of them work at the same time
+    uint32_t bytes = 0;
+    job.cluster = 0;
+    for (uint32_t cluster = 1; cluster <= 8; cluster *= 2) {
+        const uint32_t share = (job.s.col_tiles + cluster - 1) / cluster;
+        uint32_t stages = 0;
+        const uint32_t need = few_bytes(share, job.tokens, cluster, stages);
+        if (need == 0) continue;
+        if (job.cluster && (uint64_t(job.s.row_tiles) * cluster > uint64_t(dev.sms) || cluster > job.s.col_tiles)) break;
+        job.cluster = cluster, job.share = share, job.stages = stages, bytes = need;
+    }
+    if (job.cluster == 0) return ENEC_ERR_TOO_LARGE;
     static std::atomic<uint64_t> allowed{0};
-    if (!allow_shared(allowed, dev, enec_micro_few_kernel<DT, NT>, kFewMostShared)) return ENEC_ERR_CUDA;
-    const uint32_t places = uint32_t(dev.sms) / cluster;
-    job.team = few_team(job.strips, job.share, places);
-    const uint32_t per_cta = kFewWarps / job.team, needed = (job.strips + per_cta - 1) / per_cta;
+    if (!allow_shared(allowed, dev, enec_micro_few_kernel<DT>, kFewMostShared)) return ENEC_ERR_CUDA;
+    const uint32_t places = uint32_t(dev.sms) / job.cluster;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((needed < places ? needed : places) * cluster);
-    cfg.blockDim = dim3(kFewThreads);
+    cfg.gridDim = dim3((job.s.row_tiles < places ? job.s.row_tiles : places) * job.cluster);
+    cfg.blockDim = dim3(kPieceThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.x = job.cluster;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, enec_micro_few_kernel<DT, NT>, job);
+    cfg.numAttrs = job.cluster > 1 ? 2 : 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, enec_micro_few_kernel<DT>, job);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return err == cudaSuccess ? ENEC_OK : ENEC_ERR_CUDA;
 }
 
-template <int DT>
-enec_status launch_any(const FewJob& job, const MicroDevice& dev, cudaStream_t stream) {
-    return job.tokens <= 8 ? launch<DT, 1>(job, dev, stream) : job.tokens <= 16 ? launch<DT, 2>(job, dev, stream) : launch<DT, 4>(job, dev, stream);
-}
-
 }  // namespace
 
-uint32_t micro_few_most_tokens(uint32_t cols) {
-    const uint32_t share = ((cols + kUnitCols - 1) / kUnitCols + 7) / 8;
-    for (uint32_t tokens : {32u, 16u, 8u, 4u, 2u, 1u}) {
-        const int nt = tokens > 16 ? 4 : tokens > 8 ? 2 : 1;
-        if (few_fixed_bytes(nt, 1) + uint64_t(share) * few_unit_bytes(nt, tokens) <= kFewMostShared) return tokens;
-    }
-    return 0;
+bool micro_few_takes(uint32_t tokens, uint32_t col_tiles) {
+    uint32_t stages;
+    return tokens <= kPieceTokens && few_bytes((col_tiles + 7) / 8, tokens, 8, stages) != 0;
 }
 
 enec_status micro_few(const MicroProduct& p, const MicroDevice& dev, cudaStream_t stream) {
@@ -161,10 +151,8 @@ enec_status micro_few(const MicroProduct& p, const MicroDevice& dev, cudaStream_
     job.y = p.y;
     job.ld_y = p.ld_y;
     job.tokens = p.tokens;
-    const uint32_t last = p.s.rows - (p.s.row_tiles - 1) * kMicroRows;   // rows of the last record
-    job.strips = (p.s.row_tiles - 1) * 8 + (last >= 32 ? 8 : (last + 3) / 4);
     job.status = p.status;
-    return p.dt == ENEC_BF16 ? launch_any<ENEC_BF16>(job, dev, stream) : launch_any<ENEC_FP16>(job, dev, stream);
+    return p.dt == ENEC_BF16 ? launch<ENEC_BF16>(job, dev, stream) : launch<ENEC_FP16>(job, dev, stream);
 }
 
 }  // namespace enec

@@ -17,11 +17,11 @@ struct MicroProduct {
     int* status;
 };
 
-constexpr uint32_t kFewMostShared = 227 * 1024;
+constexpr uint32_t kFewMostShared = 226 * 1024;   // the kernels have a little static shared memory beside it
 constexpr uint32_t kFewHalfShared = 228 * 1024 / 2 - 1024;   // two CTAs on an SM: each has a kilobyte of the system's beside its own
 
-// The most tokens one launch for few tokens takes with rows of `cols` values (32, or fewer where they would not fit; 0 where not one does).
-uint32_t micro_few_most_tokens(uint32_t cols);
+// Whether the form for few tokens takes a call (up to 16 tokens, as long as their digits fit into a cluster's shared memory).
+bool micro_few_takes(uint32_t tokens, uint32_t col_tiles);
 enec_status micro_few(const MicroProduct& p, const MicroDevice& dev, cudaStream_t stream);
 // All tokens of the product, on the tensor cores.
 enec_status micro_many(const MicroProduct& p, const MicroDevice& dev, cudaStream_t stream);

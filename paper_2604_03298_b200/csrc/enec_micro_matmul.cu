@@ -3,8 +3,6 @@
 
 using namespace enec;
 
-constexpr uint32_t kFewTokens = 32;
-
 extern "C" enec_status enec_matmul_microscaled(const void* d_x, enec_dtype dt, size_t tokens, size_t ld_x, const void* d_w, size_t w_size,
                                                size_t rows, size_t cols, void* d_y, size_t ld_y, int* d_status, enec_stream_t stream) {
     if (dt != ENEC_BF16 && dt != ENEC_FP16) return ENEC_ERR_UNSUPPORTED_DTYPE;
@@ -27,6 +25,5 @@ extern "C" enec_status enec_matmul_microscaled(const void* d_x, enec_dtype dt, s
     p.y = static_cast<uint8_t*>(d_y);
     p.ld_y = ld_y;
     p.status = d_status;
-    const uint32_t most = micro_few_most_tokens(p.s.cols);
-    return p.tokens <= kFewTokens && p.tokens <= most ? micro_few(p, dev, stream) : micro_many(p, dev, stream);
+    return micro_few_takes(p.tokens, p.s.col_tiles) ? micro_few(p, dev, stream) : micro_many(p, dev, stream);
 }

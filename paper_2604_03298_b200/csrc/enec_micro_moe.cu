@@ -3,13 +3,14 @@
 //   l = x R^T; of the softmax p of a token's l the `top` largest, w = p or p over their sum (a pair: a token and one of its experts);
 //   h[pair] = silu(x G_e^T) * (x U_e^T);   y[token] = sum over its pairs of w (h[pair] D_e^T)
 //
-// Launch 1: every cluster of eight CTAs computes the router's products (each CTA an eighth of the columns; sums are joined through
+// Launch 1: every cluster of CTAs computes the router's products (each CTA a part of the columns; sums are joined through
 // distributed shared memory) and every CTA chooses the experts for itself, which costs less than a launch and a wait between.
-// Then it takes its share of the items (a group of pairs of one expert x a strip of 16 rows of gate and up) and writes h in fp32.
-// Launch 2 does the same over strips of down. A pair's sums go to the workspace; the CTA that is the last one to finish a strip
-// adds the pairs of every token, in the order of the token's choice, so no sum depends on which CTA that was.
-// Both are bound by the chosen experts' bytes, which are read once per group (8 or 16 pairs; see enec_micro_few.cuh for the products).
-#include "enec_micro_few.cuh"
+// Then it takes its share of the tasks: a group of pairs of one expert, a row tile of gate or of up, and all of its columns or, where
+// pairs are few, a part of them. Sums go to the workspace. Launch 2 does the same over row tiles of down; it makes the hidden values
+// from launch 1's sums as it lays out a group's columns. The CTA that is the last one to finish a row tile adds the pairs of every
+// token, in the order of the token's choice and of the parts, so no sum depends on which CTA that was.
+// Both are bound by the chosen experts' bytes, which are read once for up to 16 pairs (see enec_micro_pieces.cuh for the products).
+#include "enec_micro_pieces.cuh"
 
 #include <cooperative_groups.h>
 
@@ -21,11 +22,11 @@
 namespace enec {
 namespace {
 
-constexpr uint32_t kMoeCluster = 8;
+constexpr uint32_t kMoeCluster = 4;
+constexpr uint32_t kMoeWarps = kPieceThreads / 32;
 constexpr uint32_t kMoeMostTokens = 64;
 constexpr uint32_t kMoeMostExperts = 512;
 constexpr uint32_t kMoeMostTop = 16;
-constexpr uint32_t kMoeMostShared = kFewMostShared - 1024;   // the kernels have a little static shared memory too
 constexpr uint32_t kMoeMostLogits = 24576;   // tokens x experts: two such arrays of fp32 in shared memory
 
 struct MoeJob {
@@ -39,21 +40,21 @@ struct MoeJob {
     uint8_t* y;
     uint64_t ld_y;
     uint32_t tokens, hidden, inter, experts, top, renormalize;
-    uint32_t strips_in, strips_out;
-    uint32_t group;                  // pairs of a group, in this launch
-    uint32_t team;                   // warps of a team, in this launch
+    uint32_t group, stages;          // pairs of a group and stages of the ring, in this launch
+    uint32_t most_slices;            // parts of the columns, at most
     uint32_t ld_h;
+    uint32_t* slices;                // the parts that launch 1 has chosen
     uint32_t* pair_expert;
     float* pair_weight;
-    uint32_t* tickets;               // one per strip of down
-    float* h;
-    float* partial;
+    uint32_t* tickets;               // one per row tile of down
+    float* in_sums;                  // [part][gate, up][pair][ld_h]
+    float* out_sums;                 // [part][pair][hidden]
     int* status;
 };
 
-// Shared memory: [routing tables | sums | inverses | ring | columns]; the router's sums use what lies behind the tables.
+// Shared memory: [routing tables | ring | digits]; the router's sums use what lies behind the tables.
 __host__ __device__ inline uint32_t routing_bytes(uint32_t pairs, uint32_t experts) {
-    return (pairs * 8 + (3 * experts + 4) * 2 + 127) / 128 * 128;
+    return (pairs * 8 + (3 * experts + 4) * 2 + 1023) / 1024 * 1024;
 }
 struct Routing {
     float* weight;            // [pairs]
@@ -138,7 +139,9 @@ __device__ __forceinline__ void mma_native(float* c, const uint32_t* a0, const u
 #pragma unroll
     for (int i = 0; i < 4; i += 2) {
         if constexpr (DT == ENEC_FP16) {
-            mma_f16(c, a0[i], a1[i], a0[i + 1], a1[i + 1], b[i], b[i + 1]);
+            asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                : "r"(a0[i]), "r"(a1[i]), "r"(a0[i + 1]), "r"(a1[i + 1]), "r"(b[i]), "r"(b[i + 1]));
         } else {
             asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -165,7 +168,7 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
     const uint32_t blocks = (job.hidden + 31) / 32, share = (blocks + kMoeCluster - 1) / kMoeCluster;
     const uint32_t b0 = min(rank * share, blocks), b1 = min(b0 + share, blocks);
     const uint32_t expert_tiles = (job.experts + 15) / 16, token_tiles = (job.tokens + 7) / 8;
-    for (uint32_t unit = warp; unit < expert_tiles * token_tiles; unit += kFewWarps) {
+    for (uint32_t unit = warp; unit < expert_tiles * token_tiles; unit += kMoeWarps) {
         const uint32_t e = unit % expert_tiles * 16 + g, token = unit / expert_tiles * 8 + g;
         const uint8_t* r0 = job.router + uint64_t(e) * job.hidden * 2;
         const uint8_t* r1 = r0 + uint64_t(8) * job.hidden * 2;
@@ -197,7 +200,7 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
         for (uint32_t k = 0; k < kMoeCluster; ++k) cluster.map_shared_rank(logits, k)[i] = v;
     }
     cluster.sync();
-    for (uint32_t token = warp; token < job.tokens; token += kFewWarps) {
+    for (uint32_t token = warp; token < job.tokens; token += kMoeWarps) {
         const float* l = logits + token * job.experts;
         uint32_t taken = 0;   // bit i: expert lane + 32 i
         float highest = 0.f, sum = 0.f, mine = 0.f;
@@ -230,199 +233,193 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
     __syncthreads();
 }
 
-// The items of a CTA: [begin, end) of groups x strips, the strips of a group one after another.
-struct Share {
+// How many parts a matrix's columns are cut into: what gives the CTA with most tasks the least to do, a task counted as its records and
+// two more for taking its sums.
+__device__ __forceinline__ uint32_t choose_slices(uint64_t tasks, uint32_t records, uint32_t most) {
+    uint32_t best = 1;
+    uint64_t least = ~uint64_t(0);
+    for (uint32_t n = 1; n <= most && n <= records; n *= 2) {
+        const uint64_t cost = (tasks * n + gridDim.x - 1) / gridDim.x * ((records + n - 1) / n + 2);
+        if (cost < least) least = cost, best = n;
+    }
+    return best;
+}
+
+// The tasks of a launch, in the order group, matrix, row tile, part of the columns; and a CTA's share of them.
+struct Tasks {
+    uint32_t matrices, tiles, slices, records, share;
     uint32_t begin, end;
-};
-__device__ __forceinline__ Share share_of(uint64_t items) {
-    return {uint32_t(items * blockIdx.x / gridDim.x), uint32_t(items * (blockIdx.x + 1) / gridDim.x)};
-}
-
-// A team's walk over its CTA's items: of every group's the team's own, every teams-th one.
-struct Walk {
-    uint32_t item, end, stop;        // the next item; where the CTA's items of its group end, and all of them
-    uint32_t strips, team, teams;
-    __device__ __forceinline__ void enter(uint32_t begin) {   // the group of item `begin`
-        const uint32_t group_end = (begin / strips + 1) * strips;
-        end = min(group_end, stop);
-        item = begin + team;
-    }
-    __device__ __forceinline__ void settle() {                // on to the next group that has an item for the team
-        while (item >= end && end < stop) enter(end);
-    }
-    __device__ __forceinline__ bool more() const { return item < end; }
-};
-
-// What both kernels do: the strips of `mats` matrices (gate and up, or down) of the CTA's groups times the groups' staged columns. `rows_of`
-// gives the values of a column, `finish` takes an item's sums (of the team's warps) between two barriers of the team.
-template <int DT, int NT, int MATS, class RowOf, class Finish>
-__device__ __forceinline__ void expert_products(const Routing& r, uint32_t group, uint32_t team_warps, const uint8_t* m0, const uint8_t* m1, const MicroShape& s,
-                                                uint32_t strips, uint8_t* smem, RowOf row_of, Finish finish) {
-    constexpr uint32_t kStages = few_stages(MATS), kSums = few_sum_words(NT, MATS);
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const uint32_t units = (s.cols + kUnitCols - 1) / kUnitCols;
-    const uint32_t team = warp / team_warps, in_team = warp % team_warps, teams = kFewWarps / team_warps;
-    float* sums = reinterpret_cast<float*>(smem + few_ring_bytes(MATS)) + team * team_warps * kSums;
-    float* inverse = reinterpret_cast<float*>(smem + few_fixed_bytes(NT, MATS));
-    const uint32_t ring = smem_u32(smem) + warp * kStages * few_stage_bytes(MATS);
-    const uint32_t staged = smem_u32(inverse + units * 8 * NT);
-    const Share mine = share_of(uint64_t(r.group_first[r.experts]) * strips);
-    if (mine.begin == mine.end) return;
-    Walk asked{0, 0, mine.end, strips, team, teams};
-    asked.enter(mine.begin);
-    asked.settle();
-    uint32_t ask_u = in_team, slot = 0, ask_group = 0xFFFFFFFFu;
-    uint64_t ask_matrix = 0;
-    auto ask = [&]() {
-        if (asked.more() && ask_u < units) {
-            const uint32_t index = asked.item / strips, strip = asked.item % strips;
-            if (index != ask_group) {
-                ask_group = index;
-                ask_matrix = uint64_t(group_of(r, index, group).expert) * s.row_tiles;
-            }
-            const uint64_t at = kMicroHeaderBytes + (ask_matrix + (strip >> 3)) * s.col_tiles * kMicroRecordBytes;
-            const uint32_t stage = ring + slot * few_stage_bytes(MATS);
-            ask_unit(m0 + at, strip & 7, ask_u, stage, lane);
-            if (MATS == 2) ask_unit(m1 + at, strip & 7, ask_u, stage + few_stage_bytes(1), lane);
-            ask_u += team_warps;
-            if (ask_u >= units) {
-                ask_u = in_team;
-                asked.item += teams;
-                asked.settle();
-            }
-        }
-        cp_async_commit();
-        slot = slot + 1 == kStages ? 0 : slot + 1;
+    struct Which {
+        uint32_t group, matrix, tile, slice;
     };
-#pragma unroll
-    for (uint32_t i = 0; i < kStages - 1; ++i) ask();
-    const uint32_t values = staged + g * 64 + t * 16;
-    uint32_t from = 0;
-    Walk walk{0, 0, mine.end, strips, team, teams};
-    for (uint32_t begin = mine.begin; begin < mine.end; begin = walk.end) {
-        walk.enter(begin);
-        const Group now = group_of(r, begin / strips, group);
-        __syncthreads();   // the columns of the group before have been used
-        stage_columns<DT>([&](uint32_t i) { return row_of(r.list[now.first + i]); }, now.n, units, 0, s.cols, staged, inverse, 8 * NT);
-        __syncthreads();
-        bool exists[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) exists[nt] = nt * 8 + g < now.n;
-        for (; walk.more(); walk.item += teams) {
-            float acc[MATS][NT][4] = {};
-            for (uint32_t u = in_team; u < units; u += team_warps) {
-                cp_async_wait<kStages - 2>();
-                __syncwarp();
-                ask();   // into the slot that the unit before was read from, by all lanes
-#pragma unroll
-                for (int i = 0; i < MATS; ++i)
-                    add_unit<NT>(acc[i], ring + from * few_stage_bytes(MATS) + i * few_stage_bytes(1), values + u * 4 * now.n * 64,
-                                 inverse + u * 8 * NT + 2 * t, now.n, exists, lane);
-                from = from + 1 == kStages ? 0 : from + 1;
-            }
-#pragma unroll
-            for (int i = 0; i < MATS; ++i) put_sums<NT>(sums + in_team * kSums + i * few_sum_words(NT, 1), acc[i], lane);
-            team_sync(team, team_warps * 32);
-            finish(now, walk.item % strips, sums, in_team * 32 + lane, team);
-            team_sync(team, team_warps * 32);   // the sums have been read before they are written again
-        }
+    __device__ __forceinline__ Tasks(uint32_t groups, uint32_t matrices_, const MicroShape& s, uint32_t slices_)
+        : matrices(matrices_), tiles(s.row_tiles), slices(slices_), records(s.col_tiles), share((s.col_tiles + slices_ - 1) / slices_) {
+        const uint64_t all = uint64_t(groups) * matrices * tiles * slices;
+        begin = uint32_t(all * blockIdx.x / gridDim.x);
+        end = uint32_t(all * (blockIdx.x + 1) / gridDim.x);
     }
-    cp_async_wait<0>();
-}
+    __device__ __forceinline__ Which which(uint32_t i) const {
+        const uint32_t t = begin + i;
+        return {t / (slices * tiles * matrices), t / (slices * tiles) % matrices, t / slices % tiles, t % slices};
+    }
+    __device__ __forceinline__ PieceTask task(const Routing& r, uint32_t i, uint32_t group, const uint8_t* m0, const uint8_t* m1) const {
+        const Which w = which(i);
+        const uint64_t tile = uint64_t(group_of(r, w.group, group).expert) * tiles + w.tile;
+        const uint32_t first = min(w.slice * share, records);
+        return {(w.matrix ? m1 : m0) + kMicroHeaderBytes + tile * records * kMicroRecordBytes, first, min(share, records - first), w.group, first};
+    }
+};
 
-template <int DT, int NT>
-__global__ void __launch_bounds__(kFewThreads, 1) enec_moe_in_kernel(const __grid_constant__ MoeJob job) {
-    extern __shared__ __align__(128) uint8_t smem[];
+template <int DT>
+__global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_in_kernel(const __grid_constant__ MoeJob job) {
+    extern __shared__ uint8_t raw[];
+    __shared__ PieceShared sh;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     const uint32_t pairs = job.tokens * job.top, tables = routing_bytes(pairs, job.experts);
     const Routing r = routing_at(smem, pairs, job.experts);
+    piece_setup(sh, job.stages);
     pdl_wait();
     pdl_launch_dependents();
     route<DT>(job, r, reinterpret_cast<float*>(smem + tables));
     build_lists(r, job.group);
+    fence_async_shared();   // the ring's bulk copies go where the router's sums were
+    __syncthreads();
+    const uint32_t groups = r.group_first[job.experts];
+    const uint32_t slices = choose_slices(uint64_t(groups) * 2 * job.s_in.row_tiles, job.s_in.col_tiles, job.most_slices);
     if (blockIdx.x == 0) {
-        for (uint32_t p = threadIdx.x; p < pairs; p += kFewThreads) job.pair_expert[p] = r.expert[p], job.pair_weight[p] = r.weight[p];
-        for (uint32_t i = threadIdx.x; i < job.strips_out; i += kFewThreads) job.tickets[i] = 0;
+        for (uint32_t p = threadIdx.x; p < pairs; p += kPieceThreads) job.pair_expert[p] = r.expert[p], job.pair_weight[p] = r.weight[p];
+        for (uint32_t i = threadIdx.x; i < job.s_out.row_tiles; i += kPieceThreads) job.tickets[i] = 0;
+        if (threadIdx.x == 0) *job.slices = slices;
     }
-    if (!micro_header_ok(job.gate, job.s_in) || !micro_header_ok(job.up, job.s_in)) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
-        return;
-    }
-    expert_products<DT, NT, 2>(
-        r, job.group, job.team, job.gate, job.up, job.s_in, job.strips_in, smem + tables,
-        [&](uint32_t pair) { return job.x + uint64_t(pair / job.top) * job.ld_x * 2; },
-        [&](const Group& now, uint32_t strip, const float* sums, uint32_t thread, uint32_t) {
-            for (uint32_t i = thread; i < 16 * now.n; i += job.team * 32) {
-                const uint32_t m = i & 15, column = i >> 4;
-                const uint32_t row = (strip >> 3) * kMicroRows + strip_row(strip & 7, m);
-                float u = 0.f, v = 0.f;
-                for (uint32_t k = 0; k < job.team; ++k) {
-                    const float* theirs = sums + k * few_sum_words(NT, 2) + m * few_sum_row(NT) + column;
-                    u += theirs[0];
-                    v += theirs[few_sum_words(NT, 1)];
-                }
-                if (row < job.inter) job.h[uint64_t(r.list[now.first + column]) * job.ld_h + row] = u / (1.f + expf(-u)) * v;
+    const bool good = micro_header_ok(job.gate, job.s_in) && micro_header_ok(job.up, job.s_in);
+    const Tasks tasks(groups, 2, job.s_in, slices);
+    Group now = {};
+    const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
+    piece_products(
+        sh, smem + tables, job.stages, tasks.end - tasks.begin, job.hidden,
+        [&](uint32_t i) { return tasks.task(r, i, job.group, job.gate, job.up); },
+        [&](uint32_t i, uint32_t at) {
+            now = group_of(r, tasks.which(i).group, job.group);
+            const uint32_t columns = piece_columns(now.n), record_bytes = piece_record_bytes(now.n);
+            for (uint32_t task = worker; task < tasks.records * now.n; task += kPieceWorkers) {
+                const uint32_t k = task / now.n, c = task % now.n;
+                const uint32_t col = k * kMicroCols + 8 * lane;
+                uint32_t w[4];
+                load_eight<DT>(job.x + (uint64_t(r.list[now.first + c] / job.top) * job.ld_x + col) * 2,
+                               col < job.hidden ? int(min(job.hidden - col, 8u)) : 0, w);
+                float x[8];
+                as_floats<DT>(w, x);
+                put_digits(x, c, at + k * record_bytes, columns, lane);
             }
-        });
+        },
+        [&](uint32_t group) { return piece_columns(group_of(r, group, job.group).n); },
+        [&](uint32_t i, uint32_t tmem, bool ok) {
+            const Tasks::Which w = tasks.which(i);
+            const uint32_t row = w.tile * kMicroRows + row_in;
+            const bool any = w.slice * tasks.share < tasks.records;
+            for (uint32_t c = worker >> 2; c < now.n; c += kPieceWorkers / 4) {
+                const float v = any ? take_sum(tmem, c) : 0.f;
+                if (good && ok && row < job.inter) job.in_sums[(uint64_t(w.slice * 2 + w.matrix) * pairs + r.list[now.first + c]) * job.ld_h + row] = v;
+            }
+        },
+        [&](uint32_t) { __syncthreads(); });
+    if (threadIdx.x == 0) {
+        if (sh.failed) report(job.status, ENEC_ERR_TIMEOUT);
+        else if (!good && blockIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
+    }
 }
 
-template <int DT, int NT>
-__global__ void __launch_bounds__(kFewThreads, 1) enec_moe_out_kernel(const __grid_constant__ MoeJob job) {
-    extern __shared__ __align__(128) uint8_t smem[];
+template <int DT>
+__global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_out_kernel(const __grid_constant__ MoeJob job) {
+    extern __shared__ uint8_t raw[];
+    __shared__ PieceShared sh;
+    __shared__ uint32_t last;
     using T = typename MicroType<DT>::T;
-    __shared__ uint32_t last[kFewWarps / 4];   // of each team
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     const uint32_t pairs = job.tokens * job.top, tables = routing_bytes(pairs, job.experts);
     const Routing r = routing_at(smem, pairs, job.experts);
+    piece_setup(sh, job.stages);
     pdl_wait();
     pdl_launch_dependents();
-    for (uint32_t p = threadIdx.x; p < pairs; p += kFewThreads) r.expert[p] = uint16_t(job.pair_expert[p]), r.weight[p] = job.pair_weight[p];
-    if (!micro_header_ok(job.gate, job.s_in) || !micro_header_ok(job.up, job.s_in) || !micro_header_ok(job.down, job.s_out)) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
-        return;
-    }
+    for (uint32_t p = threadIdx.x; p < pairs; p += kPieceThreads) r.expert[p] = uint16_t(job.pair_expert[p]), r.weight[p] = job.pair_weight[p];
+    const uint32_t in_slices = *job.slices;
+    const bool good = micro_header_ok(job.gate, job.s_in) && micro_header_ok(job.up, job.s_in) && micro_header_ok(job.down, job.s_out);
     __syncthreads();
     build_lists(r, job.group);
     const uint32_t groups = r.group_first[job.experts];
-    expert_products<ENEC_FP32, NT, 1>(
-        r, job.group, job.team, job.down, nullptr, job.s_out, job.strips_out, smem + tables,
-        [&](uint32_t pair) { return reinterpret_cast<const uint8_t*>(job.h + uint64_t(pair) * job.ld_h); },
-        [&](const Group& now, uint32_t strip, const float* sums, uint32_t thread, uint32_t team) {
-            for (uint32_t i = thread; i < 16 * now.n; i += job.team * 32) {
-                const uint32_t m = i & 15, column = i >> 4, pair = r.list[now.first + column];
-                const uint32_t row = (strip >> 3) * kMicroRows + strip_row(strip & 7, m);
-                float v = 0.f;
-                for (uint32_t k = 0; k < job.team; ++k) v += sums[k * few_sum_words(NT, 1) + m * few_sum_row(NT) + column];
-                if (row < job.hidden) __stcg(job.partial + uint64_t(pair) * job.hidden + row, v * r.weight[pair]);
+    const uint32_t slices = choose_slices(uint64_t(groups) * job.s_out.row_tiles, job.s_out.col_tiles, job.most_slices);
+    const Tasks tasks(groups, 1, job.s_out, slices);
+    Group now = {};
+    const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
+    piece_products(
+        sh, smem + tables, job.stages, tasks.end - tasks.begin, job.inter,
+        [&](uint32_t i) { return tasks.task(r, i, job.group, job.down, nullptr); },
+        [&](uint32_t i, uint32_t at) {
+            now = group_of(r, tasks.which(i).group, job.group);
+            const uint32_t columns = piece_columns(now.n), record_bytes = piece_record_bytes(now.n);
+            for (uint32_t task = worker; task < tasks.records * now.n; task += kPieceWorkers) {
+                const uint32_t k = task / now.n, c = task % now.n;
+                const uint32_t col = k * kMicroCols + 8 * lane;
+                const int valid = col < job.inter ? int(min(job.inter - col, 8u)) : 0;
+                float a[8] = {}, u[8] = {};
+                for (uint32_t s = 0; s < in_slices; ++s) {
+                    const float* from = job.in_sums + (uint64_t(s * 2) * pairs + r.list[now.first + c]) * job.ld_h + col;
+                    uint32_t wa[8], wu[8];
+                    load_eight<ENEC_FP32>(reinterpret_cast<const uint8_t*>(from), valid, wa);
+                    load_eight<ENEC_FP32>(reinterpret_cast<const uint8_t*>(from + uint64_t(pairs) * job.ld_h), valid, wu);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) a[e] += __uint_as_float(wa[e]), u[e] += __uint_as_float(wu[e]);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a[e] = a[e] / (1.f + expf(-a[e])) * u[e];
+                put_digits(a, c, at + k * record_bytes, columns, lane);
             }
-            // every thread's values are visible to all before the ticket counts the item
+        },
+        [&](uint32_t group) { return piece_columns(group_of(r, group, job.group).n); },
+        [&](uint32_t i, uint32_t tmem, bool ok) {
+            const Tasks::Which w = tasks.which(i);
+            const uint32_t row = w.tile * kMicroRows + row_in;
+            const bool any = w.slice * tasks.share < tasks.records;
+            for (uint32_t c = worker >> 2; c < now.n; c += kPieceWorkers / 4) {
+                const float v = any ? take_sum(tmem, c) : 0.f;
+                const uint32_t pair = r.list[now.first + c];
+                if (row < job.hidden) __stcg(job.out_sums + (uint64_t(w.slice) * pairs + pair) * job.hidden + row, v * r.weight[pair]);
+            }
+            // every worker's values are visible to all before the ticket counts the task
             __threadfence();
-            team_sync(team, job.team * 32);
-            if (thread == 0) last[team] = atomicAdd(job.tickets + strip, 1u) == groups - 1;
-            team_sync(team, job.team * 32);
-            if (!last[team]) return;
+            asm volatile("bar.sync 1, %0;" ::"n"(kPieceWorkers * 32) : "memory");
+            if (worker == 0 && lane == 0) last = atomicAdd(job.tickets + w.tile, 1u) == groups * slices - 1;
+            asm volatile("bar.sync 1, %0;" ::"n"(kPieceWorkers * 32) : "memory");
+            if (!last || !good || !ok) return;
             __threadfence();
-            for (uint32_t i = thread; i < 16 * job.tokens; i += job.team * 32) {
-                const uint32_t m = i & 15, token = i >> 4;
-                const uint32_t row = (strip >> 3) * kMicroRows + strip_row(strip & 7, m);
-                if (row >= job.hidden) continue;
+            if (row >= job.hidden) return;
+            for (uint32_t token = worker >> 2; token < job.tokens; token += kPieceWorkers / 4) {
                 float v = 0.f;
-                for (uint32_t j = 0; j < job.top; ++j) v += __ldcg(job.partial + uint64_t(token * job.top + j) * job.hidden + row);
+                for (uint32_t j = 0; j < job.top; ++j) {
+                    for (uint32_t s = 0; s < slices; ++s) v += __ldcg(job.out_sums + (uint64_t(s) * pairs + token * job.top + j) * job.hidden + row);
+                }
                 reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
             }
-        });
+        },
+        [&](uint32_t) { __syncthreads(); });
+    if (threadIdx.x == 0) {
+        if (sh.failed) report(job.status, ENEC_ERR_TIMEOUT);
+        else if (!good && blockIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
+    }
 }
 
-uint32_t strips_of(const MicroShape& s) {
-    const uint32_t last = s.rows - (s.row_tiles - 1) * kMicroRows;
-    return (s.row_tiles - 1) * 8 + (last >= 32 ? 8 : (last + 3) / 4);
-}
-
-// Pairs per group, and with them the shared memory: as many as there may be.
-bool choose_group(uint32_t fixed, uint32_t units, int nt, uint32_t most, uint32_t least_bytes, uint32_t& group, uint32_t& bytes) {
+// Pairs per group, stages of the ring and with them the shared memory: as many pairs as there may be with four stages.
+bool choose_group(uint32_t fixed, uint32_t records, uint32_t most, uint32_t least_bytes, uint32_t& group, uint32_t& stages, uint32_t& bytes) {
     for (group = most; group > 0; --group) {
-        const uint64_t need = fixed + uint64_t(units) * few_unit_bytes(nt, group);
-        if (need > kMoeMostShared) continue;
-        bytes = need > least_bytes ? uint32_t(need) : least_bytes;
-        return bytes <= kMoeMostShared;
+        const uint64_t others = 1024 + fixed + uint64_t(records) * piece_record_bytes(group);
+        if (others + 4 * kMicroRecordBytes > kFewMostShared) continue;
+        const uint64_t fit = (kFewMostShared - others) / kMicroRecordBytes;
+        stages = fit < kPieceMostStages ? uint32_t(fit) : kPieceMostStages;
+        bytes = uint32_t(others + stages * kMicroRecordBytes);
+        if (bytes < 1024 + fixed + least_bytes) bytes = 1024 + fixed + least_bytes;
+        return bytes <= kFewMostShared;
     }
     return false;
 }
@@ -437,7 +434,7 @@ bool resident_clusters(Kernel* kernel, const MicroDevice& dev, uint32_t bytes, u
     if (n == 0) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(kMoeCluster);
-        cfg.blockDim = dim3(kFewThreads);
+        cfg.blockDim = dim3(kPieceThreads);
         cfg.dynamicSmemBytes = bytes;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -454,28 +451,24 @@ bool resident_clusters(Kernel* kernel, const MicroDevice& dev, uint32_t bytes, u
     return true;
 }
 
-template <int DT, int NT>
+template <int DT>
 enec_status launch_moe(MoeJob job, const MicroDevice& dev, cudaStream_t stream) {
     const uint32_t pairs = job.tokens * job.top, tables = routing_bytes(pairs, job.experts);
-    const uint32_t most = 8 * NT < job.tokens ? 8 * NT : job.tokens;   // an expert has at most one pair of a token
+    const uint32_t most = kPieceTokens < job.tokens ? kPieceTokens : job.tokens;   // an expert has at most one pair of a token
     uint32_t bytes = 0, clusters = 0;
     static std::atomic<uint64_t> allowed_in{0}, allowed_out{0};
-    const uint32_t units_in = (job.hidden + kUnitCols - 1) / kUnitCols, units_out = (job.inter + kUnitCols - 1) / kUnitCols;
     MoeJob second = job;
     uint32_t bytes2 = 0;
-    if (!choose_group(tables + few_fixed_bytes(NT, 2), units_in, NT, most, tables + 8 * job.tokens * job.experts, job.group, bytes) ||
-        !choose_group(tables + few_fixed_bytes(NT, 1), units_out, NT, most, 0, second.group, bytes2))
+    if (!choose_group(tables, job.s_in.col_tiles, most, 8 * job.tokens * job.experts, job.group, job.stages, bytes) ||
+        !choose_group(tables, job.s_out.col_tiles, most, 0, second.group, second.stages, bytes2))
         return ENEC_ERR_TOO_LARGE;
-    if (!allow_shared(allowed_in, dev, enec_moe_in_kernel<DT, NT>, kMoeMostShared) ||
-        !allow_shared(allowed_out, dev, enec_moe_out_kernel<DT, NT>, kMoeMostShared) ||
-        !resident_clusters(enec_moe_in_kernel<DT, NT>, dev, bytes, clusters))
+    if (!allow_shared(allowed_in, dev, enec_moe_in_kernel<DT>, kFewMostShared) ||
+        !allow_shared(allowed_out, dev, enec_moe_out_kernel<DT>, kFewMostShared) ||
+        !resident_clusters(enec_moe_in_kernel<DT>, dev, bytes, clusters))
         return ENEC_ERR_CUDA;
-    const uint64_t used = pairs < job.experts ? pairs : job.experts;   // experts with work, at most
-    job.team = few_team(used * job.strips_in, units_in, clusters * kMoeCluster);
-    second.team = few_team(used * job.strips_out, units_out, uint32_t(dev.sms));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(clusters * kMoeCluster);
-    cfg.blockDim = dim3(kFewThreads);
+    cfg.blockDim = dim3(kPieceThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -486,29 +479,31 @@ enec_status launch_moe(MoeJob job, const MicroDevice& dev, cudaStream_t stream) 
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    cudaError_t err = cudaLaunchKernelEx(&cfg, enec_moe_in_kernel<DT, NT>, job);
+    cudaError_t err = cudaLaunchKernelEx(&cfg, enec_moe_in_kernel<DT>, job);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     if (err != cudaSuccess) return ENEC_ERR_CUDA;
-    err = launch_pdl(enec_moe_out_kernel<DT, NT>, uint32_t(dev.sms), kFewThreads, bytes2, stream, second);
+    err = launch_pdl(enec_moe_out_kernel<DT>, uint32_t(dev.sms), kPieceThreads, bytes2, stream, second);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return err == cudaSuccess ? ENEC_OK : ENEC_ERR_CUDA;
 }
 
 struct MoeLayout {
-    uint64_t weight, tickets, h, partial, total;
-    uint32_t ld_h;
+    uint64_t weight, tickets, in_sums, out_sums, total;
+    uint32_t ld_h, most_slices;
 };
 bool moe_layout(uint64_t tokens, uint64_t hidden, uint64_t inter, uint64_t experts, uint64_t top, MoeLayout& l) {
     if (tokens > kMoeMostTokens || experts > kMoeMostExperts || top > kMoeMostTop || tokens * experts > kMoeMostLogits || (hidden >> 24) ||
         (inter >> 24))
         return false;
     const uint64_t pairs = tokens * top;
+    // parts of the columns only while pairs are few: with 64 pairs and more there are tasks enough
+    l.most_slices = pairs >= 64 ? 1 : pairs > 8 ? uint32_t(64 / pairs) : 8;
     l.ld_h = uint32_t((inter + 3) & ~uint64_t(3));
-    l.weight = align16(pairs * 4);
+    l.weight = 16 + align16(pairs * 4);
     l.tickets = l.weight + align16(pairs * 4);
-    l.h = l.tickets + align16((hidden + kMicroRows) / kMicroRows * 8 * 4);
-    l.partial = l.h + pairs * l.ld_h * 4;
-    l.total = l.partial + align16(pairs * hidden * 4);
+    l.in_sums = l.tickets + align16((hidden + kMicroRows) / kMicroRows * 4);
+    l.out_sums = l.in_sums + l.most_slices * 2 * pairs * l.ld_h * 4;
+    l.total = l.out_sums + align16(l.most_slices * pairs * hidden * 4);
     return true;
 }
 
@@ -557,16 +552,15 @@ extern "C" enec_status enec_moe_microscaled(const void* d_x, enec_dtype dt, size
     job.experts = uint32_t(experts);
     job.top = uint32_t(top_k);
     job.renormalize = renormalize != 0;
-    job.strips_in = strips_of(job.s_in);
-    job.strips_out = strips_of(job.s_out);
-    job.group = job.team = 0;
+    job.group = job.stages = 0;
+    job.most_slices = l.most_slices;
     job.ld_h = l.ld_h;
-    job.pair_expert = reinterpret_cast<uint32_t*>(ws);
+    job.slices = reinterpret_cast<uint32_t*>(ws);
+    job.pair_expert = reinterpret_cast<uint32_t*>(ws + 16);
     job.pair_weight = reinterpret_cast<float*>(ws + l.weight);
     job.tickets = reinterpret_cast<uint32_t*>(ws + l.tickets);
-    job.h = reinterpret_cast<float*>(ws + l.h);
-    job.partial = reinterpret_cast<float*>(ws + l.partial);
+    job.in_sums = reinterpret_cast<float*>(ws + l.in_sums);
+    job.out_sums = reinterpret_cast<float*>(ws + l.out_sums);
     job.status = d_status;
-    if (dt == ENEC_BF16) return tokens <= 8 ? launch_moe<ENEC_BF16, 1>(job, dev, stream) : launch_moe<ENEC_BF16, 2>(job, dev, stream);
-    return tokens <= 8 ? launch_moe<ENEC_FP16, 1>(job, dev, stream) : launch_moe<ENEC_FP16, 2>(job, dev, stream);
+    return dt == ENEC_BF16 ? launch_moe<ENEC_BF16>(job, dev, stream) : launch_moe<ENEC_FP16>(job, dev, stream);
 }

@@ -1,0 +1,234 @@
+// Products of a few columns with microscaled weights: what the product for few tokens and the expert layer share.
+//
+// Such a product reads every weight once and should be bound by that. Bringing the weights back costs more: two values take a conversion
+// and most of an extraction, and with all that belongs to them (mma.m16n8k16, scales, copies) a weight took so many issue slots that 8
+// tokens x 4096 x 14336 ran at 1.5 TB/s. So the weights stay as they are, and the columns are brought to the weights' format:
+//
+//   x = sum over p < 8 of d_p 8^-p 2^s, d_p in -4 .. 3
+//
+// for 32 neighbouring values with one s: balanced octal digits, all of which E2M1 has exactly, so every digit is a column of its own
+// in the 4-bit product with block scales (tcgen05.mma, kind::mxf4), its scale 2^(s - 3p). A column then costs eight columns of an
+// instruction that is far from being the bound: a record of 128 x 256 weights arrives every 750 clocks at HBM's rate, and 16 tokens
+// (128 columns) take 260. The products of digits and weights are exact; the eight sums are added in fp32, the smallest first.
+//
+// What x loses: it is rounded to 2^-22 of the largest of its 32 neighbours (all bits of a bf16 value down to 2^-14 of the largest, of an
+// fp16 value down to 2^-11). A NaN or an infinity makes its column NaN.
+//
+// A CTA takes tasks: 128 rows (a row tile of a matrix) x a range of records of columns. One warp copies records in bulk into a ring and
+// goes on to the next tasks' while results are taken; one issues the matrix instructions; sixteen make the digits and take results.
+#pragma once
+
+#include "enec_micro_mma.cuh"
+
+namespace enec {
+
+constexpr uint32_t kPieces = 8;
+constexpr uint32_t kPieceTokens = 16;        // columns of x that a CTA takes: 128 of the accumulator
+constexpr uint32_t kPieceMostStages = 8;
+constexpr uint32_t kPieceWorkers = 16;       // warps
+constexpr uint32_t kPieceThreads = (2 + kPieceWorkers) * 32;
+constexpr uint32_t kPieceTmem = 256;         // columns: 128 of sums, 16 of scales for each stage
+
+__host__ __device__ constexpr uint32_t piece_columns(uint32_t tokens) { return (tokens * kPieces + 15) / 16 * 16; }
+// A record's digits: rows of 128 bytes as a matrix operand, and 1024 bytes of scales.
+__host__ __device__ constexpr uint32_t piece_record_bytes(uint32_t tokens) { return piece_columns(tokens) * 128 + 1024; }
+
+#ifdef __CUDACC__
+
+struct PieceShared {
+    uint64_t full[kPieceMostStages], empty[kPieceMostStages], staged, done;
+    uint32_t tmem;
+    volatile int failed;
+};
+
+// Rows 128 `row_tile` .. of a matrix whose records begin at `records`, columns in records first .. first + count - 1.
+struct PieceTask {
+    const uint8_t* records;
+    uint32_t first, count;
+    uint32_t group;        // tasks of the same group use the same digits
+    uint32_t digits;       // of the staged records the one that belongs to `first`
+};
+
+__device__ __forceinline__ void piece_setup(PieceShared& sh, uint32_t stages) {
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < stages; ++i) mbar_init(sh.full + i, 1), mbar_init(sh.empty + i, 1);
+        mbar_init(&sh.staged, kPieceWorkers * 32);
+        mbar_init(&sh.done, 1);
+        mbar_fence_init();
+        sh.failed = 0;
+    }
+    if (threadIdx.x >> 5 == 1) tmem_alloc(&sh.tmem, kPieceTmem);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+}
+
+// Eight values of a block (a quarter of it; the quarters are four neighbouring lanes) to eight words of eight digits' codes, digit p of the
+// eight in word p; returns the scale byte of digit 0 (digit p's is 3p less), 255 where the block holds a NaN or an infinity.
+__device__ __forceinline__ uint32_t make_digits(const float* x, uint32_t* words) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+    // the largest magnitude goes to 2^21 .. 2^22 of 8 octal digits, whose largest is 3 (8^8 - 1) / 7 > 2^22; one digit's worth of the first
+    // is 8^7 = 2^21, so the first scale is the largest's power of two
+    const uint32_t field = min(max(top >> 23, 22u), 254u);            // below: the factor stays, and with it the absolute error
+    const float factor = __uint_as_float((127 + 21 + 127 - field) << 23);
+    uint32_t v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        // 1.5 x 2^23 + X, X rounded to a whole number; then X + 4 (8^8 - 1) / 7, whose octal digits are d + 4
+        uint32_t o = __float_as_uint(fmaf(x[i], factor, 12582912.f)) - 0x4B400000u + 044444444u;
+        // three bits each to four bits each
+        o = (o & 0x00000FFFu) | ((o & 0x00FFF000u) << 4);
+        o = (o & 0x003F003Fu) | ((o & 0x0FC00FC0u) << 2);
+        o = (o & 0x07070707u) | ((o & 0x38383838u) << 1);
+        // d + 4 -> the code of d: four nibbles choose among eight bytes
+        const uint32_t a = prmt(0x0A0C0D0Eu, 0x05040200u, o), b = prmt(0x0A0C0D0Eu, 0x05040200u, o >> 16);
+        v[i] = prmt(a | (a >> 4), b | (b >> 4), 0x6420);
+    }
+    // 8 x 8 nibbles: from a word per value to a word per digit; digit 0 is the highest nibble
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const uint32_t a = v[i], b = v[i + 1];
+        v[i] = select_bits(0x0F0F0F0Fu, a, b << 4);              // nibble 2j: values i, i + 1 of digits 7 - 2j
+        v[i + 1] = select_bits(0x0F0F0F0Fu, a >> 4, b);          // of digits 6 - 2j
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        // bytes 0 .. 3 of v[i], v[i + 2], v[i + 4], v[i + 6] are digits 7 - i, 5 - i, 3 - i, 1 - i of two values each
+        const uint32_t lo0 = prmt(v[i], v[i + 2], 0x5140), lo1 = prmt(v[i + 4], v[i + 6], 0x5140);
+        const uint32_t hi0 = prmt(v[i], v[i + 2], 0x7362), hi1 = prmt(v[i + 4], v[i + 6], 0x7362);
+        words[7 - i] = prmt(lo0, lo1, 0x5410);
+        words[5 - i] = prmt(lo0, lo1, 0x7632);
+        words[3 - i] = prmt(hi0, hi1, 0x5410);
+        words[1 - i] = prmt(hi0, hi1, 0x7632);
+    }
+    return top >= 0x7F800000u ? 255u : field;
+}
+
+// One warp: the digits of a column's 256 values of one record (eight a lane) to the operand and its scales.
+__device__ __forceinline__ void put_digits(const float* x, uint32_t column, uint32_t record, uint32_t columns16, uint32_t lane) {
+    uint32_t words[8];
+    const uint32_t byte = make_digits(x, words);
+    const uint32_t chunk = lane >> 2, part = lane & 3;
+    const uint32_t row = record + column * kPieces * 128 + part * 4;
+#pragma unroll
+    for (uint32_t p = 0; p < kPieces; ++p) sts32(row + p * 128 + ((chunk ^ p) << 4), byte == 255 ? 0u : words[p]);
+    // each lane of a block stores two of the eight scales
+    const uint32_t scales = record + columns16 * 128 + (chunk >> 2) * 512 + (chunk & 3);
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        const uint32_t p = 2 * part + i, c = column * kPieces + p;
+        const uint32_t scale = byte == 255 ? 255u : byte > 3 * p ? byte - 3 * p : 0u;
+        asm volatile("st.shared.u8 [%0], %1;" ::"r"(scales + (c & 31) * 16 + (c >> 5) * 4), "r"(scale) : "memory");
+    }
+}
+
+// The sum of a column's eight digits for this lane's row.
+__device__ __forceinline__ float take_sum(uint32_t tmem, uint32_t column) {
+    uint32_t v[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(tmem + column * kPieces));
+    tmem_load_wait();
+    float sum = 0.f;
+#pragma unroll
+    for (int p = kPieces - 1; p >= 0; --p) sum += __uint_as_float(v[p]);
+    return sum;
+}
+
+// All roles of a CTA over its tasks. task_of(i): the i-th. stage(i, at): called by the workers' warps where a group begins, writes the
+// digits of its records to `at` on. columns_of(group): columns of the accumulator it has, a multiple of 16. finish(i, tmem, ok): by the
+// workers, takes the sums from their lanes of tensor memory; where not ok, a wait has run out and they are nothing. meet(i): where all threads meet behind every task. smem: the ring, then the
+// digits. cols: of the matrices. sh.failed is set where a wait ran out.
+template <class TaskOf, class Stage, class ColumnsOf, class Finish, class Meet>
+__device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, uint32_t stages, uint32_t n_tasks, uint32_t cols, TaskOf task_of,
+                                               Stage stage, ColumnsOf columns_of, Finish finish, Meet meet) {
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t ring = smem_u32(smem), digits = ring + stages * kMicroRecordBytes;
+    const uint32_t tmem = sh.tmem;
+    uint32_t group = 0xFFFFFFFFu, groups = 0, columns = 0;
+    uint32_t used = 0;                                        // records of the tasks so far
+    uint32_t ask_task = 0, ask_record = 0, asked = 0;         // the copying warp's
+    for (uint32_t i = 0; i < n_tasks; ++i) {
+        const PieceTask task = task_of(i);
+        const bool begins = task.group != group;
+        if (begins) group = task.group, ++groups, columns = columns_of(group);
+        const uint32_t after = used + task.count;
+        if (warp == 0) {
+            if (lane == 0) {
+                // all of this task's records, and of the next ones' as many as the ring takes once these are used
+                while (ask_task < n_tasks && asked < after + stages && !sh.failed) {
+                    const PieceTask t = ask_task == i ? task : task_of(ask_task);
+                    if (ask_record >= t.count) {
+                        ++ask_task, ask_record = 0;
+                        continue;
+                    }
+                    const uint32_t s = asked % stages;
+                    if (asked >= stages && !suspended_wait(sh.empty + s, (asked / stages - 1) & 1, &sh.failed)) {
+                        sh.failed = 1;
+                        break;
+                    }
+                    mbar_expect_tx(sh.full + s, kMicroRecordBytes);
+                    bulk_g2s(smem + s * kMicroRecordBytes, t.records + uint64_t(t.first + ask_record) * kMicroRecordBytes, kMicroRecordBytes,
+                             sh.full + s);
+                    ++asked, ++ask_record;
+                }
+            }
+        } else if (warp == 1) {
+            if (lane == 0) {
+                const uint32_t idesc = scaled_idesc(columns);
+                if (begins && !suspended_wait(&sh.staged, (groups - 1) & 1, &sh.failed)) sh.failed = 1;
+                for (uint32_t k = 0; k < task.count && !sh.failed; ++k) {
+                    const uint32_t at = used + k, s = at % stages;
+                    if (!suspended_wait(sh.full + s, (at / stages) & 1, &sh.failed)) {
+                        sh.failed = 1;
+                        break;
+                    }
+                    tcgen05_fence_after();
+                    const uint32_t a = ring + s * kMicroRecordBytes, b = digits + (task.digits + k) * (columns * 128 + 1024);
+                    const uint32_t to = tmem + kPieceTokens * kPieces + s * 16;
+#pragma unroll
+                    for (uint32_t h = 0; h < 2; ++h) {
+                        copy_scales(to + h * 4, scale_desc(a + kMicroElemBytes + h * 512));
+                        copy_scales(to + 8 + h * 4, scale_desc(b + columns * 128 + h * 512));
+                    }
+                    const uint32_t steps = min(4u, (cols - (task.first + k) * kMicroCols + 63) / 64);
+                    for (uint32_t q = 0; q < steps; ++q) {
+                        const uint32_t h = q >> 1, pair = (q & 1) * 2;
+                        mma_scaled(tmem, operand_desc(a + q * 32), operand_desc(b + q * 32), idesc | pair << 4 | pair << 29, to + h * 4, to + 8 + h * 4,
+                                   k > 0 || q > 0);
+                    }
+                    tcgen05_commit(sh.empty + s);
+                }
+                tcgen05_commit(&sh.done);
+                mbar_wait_bounded(&sh.done, i & 1);   // no instruction may be under way when tensor memory is given back
+            }
+        } else {
+            if (begins) {
+                stage(i, digits);
+                fence_async_shared();
+                mbar_arrive(&sh.staged);
+            }
+            if (!suspended_wait(&sh.done, i & 1, &sh.failed)) sh.failed = 1;
+            tcgen05_fence_after();
+            finish(i, tmem + ((warp & 3) * 32 << 16), !sh.failed);
+            tcgen05_fence_before();
+        }
+        used = after;
+        meet(i);
+        tcgen05_fence_after();
+    }
+    if (warp == 0 && lane == 0) {   // nothing may be in flight when the CTA ends
+        for (uint32_t k = asked > stages ? asked - stages : 0; k < asked; ++k) mbar_wait_bounded(sh.full + k % stages, (k / stages) & 1);
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_free(tmem, kPieceTmem);
+}
+
+#endif  // __CUDACC__
+
+}  // namespace enec

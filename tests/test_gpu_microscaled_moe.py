@@ -5,7 +5,7 @@ import torch
 
 import microscaled_reference as ref
 from gpu_util import status_tensor
-from test_gpu_microscaled import DTYPES, HALF_STEP, enec, strided
+from test_gpu_microscaled import DTYPES, HALF_STEP, block_tops, enec, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -27,9 +27,9 @@ def undecided(x, router, top):
 
 
 def bound_of(x, router, gate, up, down, top, renormalize, dt, chosen=None):
-    """The layer in 64 bits and how far each value may be off. Sums of n terms in fp32: n 2^-24 of the magnitudes' sum.
-    |silu'| <= 1.1; expf, the division and the products of fp32 add 2^-21 of a value at most; the hidden values are rounded to 11 bits
-    (2^-12) or, far below the largest, by 2^-25 of 2^14 (2^-39 of the largest)."""
+    """The layer in 64 bits and how far each value may be off. Products as in test_gpu_microscaled.product_bound: operands to 2^-22 of the
+    largest of their block, sums of n terms in fp32 to 3 n 2^-24 of the magnitudes' sum; sums of parts of the columns add up to 8 more
+    roundings. |silu'| <= 1.1; expf, the division and the products of fp32 add 2^-21 of a value at most."""
     e24 = 2.0 ** -24
     want, chosen = ref.layer(x, router, gate, up, down, top, renormalize, chosen)
     tokens, hidden = x.shape
@@ -39,17 +39,18 @@ def bound_of(x, router, gate, up, down, top, renormalize, dt, chosen=None):
     p = np.exp(logits - logits.max(-1, keepdims=True))
     p /= p.sum(-1, keepdims=True)
     off = np.zeros_like(want)
+    x_off = 2.0 ** -22 * block_tops(x)
     for t in range(tokens):
         w = p[t, chosen[t]]
         w = w / w.sum() if renormalize else w
         for e, share in zip(chosen[t], w):
             a, u = gate[e] @ x[t], up[e] @ x[t]
-            a_off, u_off = ((hidden + 16) * e24 * (np.abs(m[e]) @ np.abs(x[t])) for m in (gate, up))
+            a_off, u_off = (np.abs(m[e]) @ (x_off[t] + 3 * (hidden + 24) * e24 * (np.abs(x[t]) + x_off[t])) for m in (gate, up))
             h = silu(a) * u
-            h_off = (1.1 * a_off * (np.abs(u) + u_off) + (np.abs(silu(a)) + 1.1 * a_off) * u_off + 2.0 ** -21 * np.abs(h)
-                     + 2.0 ** -12 * np.abs(h) + 2.0 ** -39 * np.abs(h).max())
+            h_off = 1.1 * a_off * (np.abs(u) + u_off) + (np.abs(silu(a)) + 1.1 * a_off) * u_off + 2.0 ** -21 * np.abs(h)
+            rounding = 2.0 ** -22 * block_tops(np.abs(h) + h_off)
             part = down[e] @ h
-            part_off = np.abs(down[e]) @ h_off + (inter + 16) * e24 * (np.abs(down[e]) @ np.abs(h))
+            part_off = np.abs(down[e]) @ (h_off + rounding + 3 * (inter + 24) * e24 * (np.abs(h) + h_off + rounding))
             off[t] += share * (part_off + (4 * logit_off[t] + 2.0 ** -20) * (np.abs(part) + part_off))
     tiny = torch.finfo(DTYPES[dt]).smallest_normal * HALF_STEP[dt]
     return want, off + HALF_STEP[dt] * (np.abs(want) + off) + tiny
@@ -133,8 +134,8 @@ def test_all_experts_of_one_and_many_experts():
 
 def test_long_rows():
     """Rows of which eight do not fit beside one another: smaller groups, both in front of and behind the activation."""
-    check(8, 9000, 64, 2, 1, 0)
-    check(8, 64, 20000, 2, 1, 1)
+    check(16, 9000, 64, 2, 1, 0)
+    check(16, 64, 9001, 2, 1, 1)
 
 
 def test_ties_go_to_the_lower_expert():
