@@ -66,20 +66,21 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
     const uint8_t* xr = job.x + kMicroHeaderBytes + uint64_t(x_tile) * records * kMicroRecordBytes;
     const uint64_t strip = uint64_t(records) * kMicroRecordBytes;
 
+    const uint32_t leader = elected();
     if (warp == 0) {
-        if (lane == 0) {
-            const uint32_t bytes = mt * kMicroRecordBytes + first_rows * 128 + 1024 + (second ? (n - first_rows) * 128 + 1024 : 0);
-            uint32_t k = 0;
-            for (; k < records; ++k) {
-                const uint32_t s = k % kBothStages;
-                if (k >= kBothStages && !mbar_wait_bounded(empty + s, (k / kBothStages - 1) & 1)) {
-                    failed = 1;
-                    break;
-                }
-                uint8_t* a = smem + s * stage_bytes;
-                uint8_t* b = a + MT * kMicroElemBytes;
-                uint8_t* scales = b + n * 128;
-                const uint64_t at = uint64_t(k) * kMicroRecordBytes;
+        const uint32_t bytes = mt * kMicroRecordBytes + first_rows * 128 + 1024 + (second ? (n - first_rows) * 128 + 1024 : 0);
+        uint32_t k = 0;
+        for (; k < records; ++k) {
+            const uint32_t s = k % kBothStages;
+            if (k >= kBothStages && !suspended_wait(empty + s, (k / kBothStages - 1) & 1, &failed)) {
+                failed = 1;
+                break;
+            }
+            uint8_t* a = smem + s * stage_bytes;
+            uint8_t* b = a + MT * kMicroElemBytes;
+            uint8_t* scales = b + n * 128;
+            const uint64_t at = uint64_t(k) * kMicroRecordBytes;
+            if (leader) {
                 mbar_expect_tx(full + s, bytes);
                 for (uint32_t i = 0; i < mt; ++i) {
                     bulk_g2s(a + i * kMicroElemBytes, wr + i * strip + at, kMicroElemBytes, full + s);
@@ -92,48 +93,46 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
                     bulk_g2s(scales + MT * 1024 + 1024, xr + strip + at + kMicroElemBytes, 1024, full + s);
                 }
             }
-            // nothing may be in flight when the CTA ends
-            for (uint32_t i = k > kBothStages ? k - kBothStages : 0; i < k; ++i) mbar_wait_bounded(full + i % kBothStages, (i / kBothStages) & 1);
         }
+        // nothing may be in flight when the CTA ends
+        for (uint32_t i = k > kBothStages ? k - kBothStages : 0; i < k; ++i) mbar_wait_bounded(full + i % kBothStages, (i / kBothStages) & 1);
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = scaled_idesc(n);
-            for (uint32_t k = 0; k < records; ++k) {
-                const uint32_t s = k % kBothStages;
-                if (!mbar_wait_bounded(full + s, (k / kBothStages) & 1)) {
-                    failed = 1;
-                    break;
-                }
-                tcgen05_fence_after();
-                const uint32_t a = smem_u32(smem) + s * stage_bytes, b = a + MT * kMicroElemBytes, scales = b + n * 128;
-                // tensor memory of a stage's scales: of the columns' four chunks h, 4 columns per 128 rows of W, and 8 for the tokens
-                const uint32_t to = tmem + MT * kBothMostTokens + s * kScaleColumns;
-#pragma unroll
-                for (uint32_t h = 0; h < 2; ++h) {
-#pragma unroll
-                    for (uint32_t i = 0; i < MT; ++i)
-                        if (i < mt) copy_scales(to + (2 * i + h) * 4, scale_desc(scales + i * 1024 + h * 512));
-                    copy_scales(to + MT * 8 + h * 8, scale_desc(scales + MT * 1024 + h * 512));
-                    if (second) copy_scales(to + MT * 8 + h * 8 + 4, scale_desc(scales + (MT + 1) * 1024 + h * 512));
-                }
-                const uint32_t steps = min(4u, (job.sw.cols - k * kMicroCols + 63) / 64);
-                for (uint32_t q = 0; q < steps; ++q) {
-                    const uint32_t h = q >> 1, pair = (q & 1) * 2;
-                    const uint32_t scale_x = to + MT * 8 + h * 8 + skip / 32;
-#pragma unroll
-                    for (uint32_t i = 0; i < MT; ++i)
-                        if (i < mt)
-                            mma_scaled(tmem + i * kBothMostTokens, operand_desc(a + i * kMicroElemBytes + q * 32), operand_desc(b + q * 32),
-                                       idesc | pair << 4 | pair << 29, to + (2 * i + h) * 4, scale_x, k > 0 || q > 0);
-                }
-                tcgen05_commit(empty + s);
+        const uint32_t idesc = scaled_idesc(n);
+        const uint64_t operands = operand_desc(smem_u32(smem)), scales = scale_desc(smem_u32(smem) + MT * kMicroElemBytes + n * 128);
+        for (uint32_t k = 0; k < records; ++k) {
+            const uint32_t s = k % kBothStages;
+            if (!suspended_wait(full + s, (k / kBothStages) & 1, &failed)) {
+                failed = 1;
+                break;
             }
-            tcgen05_commit(&done);
-            mbar_wait_bounded(&done, 0);   // no instruction may be under way when tensor memory is given back
+            tcgen05_fence_after();
+            const uint64_t a = operands + s * (stage_bytes / 16), b = a + MT * (kMicroElemBytes / 16), sc = scales + s * (stage_bytes / 16);
+            // tensor memory of a stage's scales: of the columns' four chunks h, 4 columns per 128 rows of W, and 8 for the tokens
+            const uint32_t to = tmem + MT * kBothMostTokens + s * kScaleColumns;
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+#pragma unroll
+                for (uint32_t i = 0; i < MT; ++i) copy_scales(i < mt ? leader : 0, to + (2 * i + h) * 4, sc + i * 64 + h * 32);
+                copy_scales(leader, to + MT * 8 + h * 8, sc + MT * 64 + h * 32);
+                copy_scales(second ? leader : 0, to + MT * 8 + h * 8 + 4, sc + (MT + 1) * 64 + h * 32);
+            }
+            const uint32_t steps = (job.sw.cols - k * kMicroCols + 63) / 64;
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                const uint32_t h = q >> 1, pair = (q & 1) * 2;
+                const uint32_t scale_x = to + MT * 8 + h * 8 + skip / 32;
+#pragma unroll
+                for (uint32_t i = 0; i < MT; ++i)
+                    mma_scaled(q < steps && i < mt ? leader : 0, tmem + i * kBothMostTokens, a + i * (kMicroElemBytes / 16) + q * 2, b + q * 2,
+                               idesc | pair << 4 | pair << 29, to + (2 * i + h) * 4, scale_x, k > 0 || q > 0);
+            }
+            tcgen05_commit(leader, empty + s);
         }
+        tcgen05_commit(leader, &done);
+        mbar_wait_bounded(&done, 0);   // no instruction may be under way when tensor memory is given back
     } else {
         const bool good = micro_header_ok(job.w, job.sw) && micro_header_ok(job.x, job.sx);
-        if (!mbar_wait_bounded(&done, 0)) failed = 1;
+        if (!suspended_wait(&done, 0, &failed)) failed = 1;
         tcgen05_fence_after();
         const uint32_t quarter = warp & 3;   // the lanes of tensor memory that this warp may read
         const bool wide = (job.ld_y & 1) == 0;

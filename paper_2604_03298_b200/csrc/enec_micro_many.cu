@@ -124,45 +124,43 @@ __global__ void __launch_bounds__(kManyThreads, MT == 1 ? 2 : 1) enec_micro_many
     uint8_t* raw = b_ring + kStagesB * n * 128;
     const bool good = micro_header_ok(job.w, job.s);
 
+    const uint32_t leader = elected();
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t k = 0;
-            for (; k < records; ++k) {
-                if (k > 0 && !suspended_wait(&raw_empty, (k - 1) & 1, const_cast<volatile int*>(&failed))) {
-                    failed = 1;
-                    break;
-                }
+        uint32_t k = 0;
+        for (; k < records; ++k) {
+            if (k > 0 && !suspended_wait(&raw_empty, (k - 1) & 1, &failed)) {
+                failed = 1;
+                break;
+            }
+            if (leader) {
                 mbar_expect_tx(&raw_full, mt * kMicroRecordBytes);
                 for (uint32_t i = 0; i < mt; ++i)
                     bulk_g2s(raw + i * kMicroRecordBytes, wr + i * strip + uint64_t(k) * kMicroRecordBytes, kMicroRecordBytes, &raw_full);
             }
-            if (k > 0) mbar_wait_bounded(&raw_full, (k - 1) & 1);   // nothing may be in flight when the CTA ends
         }
+        if (k > 0) mbar_wait_bounded(&raw_full, (k - 1) & 1);   // nothing may be in flight when the CTA ends
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = idesc_16bit(DT == ENEC_BF16, n);
-            for (uint32_t j = 0; j < steps; ++j) {
-                const uint32_t sa = j % kStagesA, sb = j % kStagesB;
-                if (!suspended_wait(full_a + sa, (j / kStagesA) & 1, &failed) || !suspended_wait(full_b + sb, (j / kStagesB) & 1, &failed)) {
-                    failed = 1;
-                    break;
-                }
-                tcgen05_fence_after();
-                const uint32_t a = smem_u32(a_ring) + sa * MT * 16384, b = smem_u32(b_ring) + sb * n * 128;
-#pragma unroll
-                for (uint32_t i = 0; i < MT; ++i) {
-                    if (i < mt) {
-#pragma unroll
-                        for (uint32_t q = 0; q < 4; ++q)
-                            mma_16bit(tmem + i * n, operand_desc(a + i * 16384 + q * 32), operand_desc(b + q * 32), idesc, j > 0 || q > 0);
-                    }
-                }
-                tcgen05_commit(empty_a + sa);
-                tcgen05_commit(empty_b + sb);
+        const uint32_t idesc = idesc_16bit(DT == ENEC_BF16, n);
+        const uint64_t a0 = operand_desc(smem_u32(a_ring)), b0 = operand_desc(smem_u32(b_ring));
+        for (uint32_t j = 0; j < steps; ++j) {
+            const uint32_t sa = j % kStagesA, sb = j % kStagesB;
+            if (!suspended_wait(full_a + sa, (j / kStagesA) & 1, &failed) || !suspended_wait(full_b + sb, (j / kStagesB) & 1, &failed)) {
+                failed = 1;
+                break;
             }
-            tcgen05_commit(&done);
-            mbar_wait_bounded(&done, 0);   // no instruction may be under way when tensor memory is given back
+            tcgen05_fence_after();
+            const uint64_t a = a0 + sa * (MT * 1024), b = b0 + sb * n * 8;
+#pragma unroll
+            for (uint32_t i = 0; i < MT; ++i) {
+#pragma unroll
+                for (uint32_t q = 0; q < 4; ++q)
+                    mma_16bit(i < mt ? leader : 0, tmem + i * n, a + i * 1024 + q * 2, b + q * 2, idesc, j > 0 || q > 0);
+            }
+            tcgen05_commit(leader, empty_a + sa);
+            tcgen05_commit(leader, empty_b + sb);
         }
+        tcgen05_commit(leader, &done);
+        mbar_wait_bounded(&done, 0);   // no instruction may be under way when tensor memory is given back
     } else if (warp < kFirstW) {
         // x: eight lanes a row of 64 columns
         const uint32_t me = threadIdx.x - kFirstX * 32, c = me & 7;

@@ -1,5 +1,9 @@
-// tcgen05 in the form the products of many tokens use it: one CTA per tile, accumulators in tensor memory, operands in shared memory,
-// K-major with rows of 128 bytes whose 16-byte chunks are exchanged by the row's number mod 8.
+// tcgen05 in the form the products use it: one CTA per tile, accumulators in tensor memory, operands in shared memory, K-major
+// with rows of 128 bytes whose 16-byte chunks are exchanged by the row's number mod 8.
+//
+// One thread issues. The whole warp runs its loop, waits included, and the issuing instructions are predicated on the elected lane: so
+// control flow and descriptors stay uniform. With the loop inside a branch for one lane every descriptor goes through a vector
+// register first, and a record of 8 matrix and 8 copy instructions took 3800 clocks instead of 800.
 #pragma once
 
 #include "enec_micro.cuh"
@@ -17,9 +21,19 @@ __device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns) {    
 }
 __device__ __forceinline__ void tcgen05_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tcgen05_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// One lane of the warp, the same one at every call.
+__device__ __forceinline__ uint32_t elected() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e;
+}
 // Arrives on `bar` when all tcgen05 operations that this thread has issued are done.
-__device__ __forceinline__ void tcgen05_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+__device__ __forceinline__ void tcgen05_commit(uint32_t leader, uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %1, 0;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)),
+        "r"(leader)
+        : "memory");
 }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -32,29 +46,34 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
     return uint64_t((addr & 0x3FFFF) >> 4) | uint64_t(1) << 16 | uint64_t(128 >> 4) << 32 | uint64_t(1) << 46;
 }
 // Those 512 bytes to four columns of tensor memory, the same for all four groups of 32 lanes.
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+__device__ __forceinline__ void copy_scales(uint32_t leader, uint32_t tmem, uint64_t desc) {
+    asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %2, 0;\n\t@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem), "l"(desc),
+                 "r"(leader)
+                 : "memory");
 }
 
 // D (128 rows x n columns) (+)= A B^T over 64 columns of E2M1 with one scale per 32.
-__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, bool add) {
+__device__ __forceinline__ void mma_scaled(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b,
+                                           bool add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, e;\n\t"
         "setp.ne.u32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(uint32_t(add))
+        "setp.ne.u32 e, %7, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(uint32_t(add)), "r"(leader)
         : "memory");
 }
 // E2M1 operands (1), E8M0 scales (bit 23), both K-major; the pair of scale bytes in their words goes in at bits 4 (B) and 29 (A).
 __device__ __forceinline__ uint32_t scaled_idesc(uint32_t n) { return 1u << 7 | 1u << 10 | (n >> 3) << 17 | 1u << 23 | 1u << 27; }
 
 // D (128 rows x n columns) (+)= A B^T over 16 columns of bf16 or fp16, fp32 sums.
-__device__ __forceinline__ void mma_16bit(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void mma_16bit(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, e;\n\t"
         "setp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+        "setp.ne.u32 e, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add)), "r"(leader)
         : "memory");
 }
 // fp32 sums (bit 4), bf16 (1) or fp16 (0) operands, both K-major, 128 rows.

@@ -150,62 +150,68 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
     const uint32_t ring = smem_u32(smem), digits = ring + stages * kMicroRecordBytes;
     const uint32_t tmem = sh.tmem;
     uint32_t group = 0xFFFFFFFFu, groups = 0, columns = 0;
-    uint32_t used = 0;                                        // records of the tasks so far
-    uint32_t ask_task = 0, ask_record = 0, asked = 0;         // the copying warp's
+    uint32_t used = 0;                                                  // records of the tasks so far
+    uint32_t ask_task = 0, ask_record = 0, asked = 0, ask_slot = 0, ask_phase = 0;   // the copying warp's
+    PieceTask asking = n_tasks ? task_of(0) : PieceTask{};
+    uint32_t slot = 0, phase = 0;                                       // of the record that the matrix instructions take next
+    const uint32_t leader = elected();
+    const uint64_t ring_desc = operand_desc(ring), ring_scales_desc = scale_desc(ring + kMicroElemBytes);
+    const uint64_t digits_desc = operand_desc(digits), digit_scales_desc = scale_desc(digits);
+    volatile int never = 0;
     for (uint32_t i = 0; i < n_tasks; ++i) {
         const PieceTask task = task_of(i);
         const bool begins = task.group != group;
         if (begins) group = task.group, ++groups, columns = columns_of(group);
         const uint32_t after = used + task.count;
         if (warp == 0) {
-            if (lane == 0) {
-                // all of this task's records, and of the next ones' as many as the ring takes once these are used
-                while (ask_task < n_tasks && asked < after + stages && !sh.failed) {
-                    const PieceTask t = ask_task == i ? task : task_of(ask_task);
-                    if (ask_record >= t.count) {
-                        ++ask_task, ask_record = 0;
-                        continue;
-                    }
-                    const uint32_t s = asked % stages;
-                    if (asked >= stages && !suspended_wait(sh.empty + s, (asked / stages - 1) & 1, &sh.failed)) {
-                        sh.failed = 1;
-                        break;
-                    }
-                    mbar_expect_tx(sh.full + s, kMicroRecordBytes);
-                    bulk_g2s(smem + s * kMicroRecordBytes, t.records + uint64_t(t.first + ask_record) * kMicroRecordBytes, kMicroRecordBytes,
-                             sh.full + s);
-                    ++asked, ++ask_record;
+            // all of this task's records, and of the next ones' as many as the ring takes once these are used
+            while (ask_task < n_tasks && asked < after + stages && !sh.failed) {
+                if (ask_record >= asking.count) {
+                    if (++ask_task < n_tasks) asking = task_of(ask_task);
+                    ask_record = 0;
+                    continue;
                 }
+                if (asked >= stages && !suspended_wait(sh.empty + ask_slot, ask_phase ^ 1, &sh.failed)) {
+                    sh.failed = 1;
+                    break;
+                }
+                if (leader) {
+                    mbar_expect_tx(sh.full + ask_slot, kMicroRecordBytes);
+                    bulk_g2s(smem + ask_slot * kMicroRecordBytes, asking.records + uint64_t(asking.first + ask_record) * kMicroRecordBytes,
+                             kMicroRecordBytes, sh.full + ask_slot);
+                }
+                ++asked, ++ask_record;
+                if (++ask_slot == stages) ask_slot = 0, ask_phase ^= 1;
             }
         } else if (warp == 1) {
-            if (lane == 0) {
-                const uint32_t idesc = scaled_idesc(columns);
-                if (begins && !suspended_wait(&sh.staged, (groups - 1) & 1, &sh.failed)) sh.failed = 1;
-                for (uint32_t k = 0; k < task.count && !sh.failed; ++k) {
-                    const uint32_t at = used + k, s = at % stages;
-                    if (!suspended_wait(sh.full + s, (at / stages) & 1, &sh.failed)) {
-                        sh.failed = 1;
-                        break;
-                    }
-                    tcgen05_fence_after();
-                    const uint32_t a = ring + s * kMicroRecordBytes, b = digits + (task.digits + k) * (columns * 128 + 1024);
-                    const uint32_t to = tmem + kPieceTokens * kPieces + s * 16;
-#pragma unroll
-                    for (uint32_t h = 0; h < 2; ++h) {
-                        copy_scales(to + h * 4, scale_desc(a + kMicroElemBytes + h * 512));
-                        copy_scales(to + 8 + h * 4, scale_desc(b + columns * 128 + h * 512));
-                    }
-                    const uint32_t steps = min(4u, (cols - (task.first + k) * kMicroCols + 63) / 64);
-                    for (uint32_t q = 0; q < steps; ++q) {
-                        const uint32_t h = q >> 1, pair = (q & 1) * 2;
-                        mma_scaled(tmem, operand_desc(a + q * 32), operand_desc(b + q * 32), idesc | pair << 4 | pair << 29, to + h * 4, to + 8 + h * 4,
-                                   k > 0 || q > 0);
-                    }
-                    tcgen05_commit(sh.empty + s);
+            const uint32_t idesc = scaled_idesc(columns), record16 = columns * 8 + 64;   // a record's digits in units of 16 bytes
+            if (begins && !suspended_wait(&sh.staged, (groups - 1) & 1, &sh.failed)) sh.failed = 1;
+            uint64_t b = digits_desc + task.digits * record16, bs = digit_scales_desc + columns * 8 + task.digits * record16;
+            for (uint32_t k = 0; k < task.count && !sh.failed; ++k) {
+                if (!suspended_wait(sh.full + slot, phase, &sh.failed)) {
+                    sh.failed = 1;
+                    break;
                 }
-                tcgen05_commit(&sh.done);
-                mbar_wait_bounded(&sh.done, i & 1);   // no instruction may be under way when tensor memory is given back
+                tcgen05_fence_after();
+                const uint64_t a = ring_desc + slot * (kMicroRecordBytes / 16), as = ring_scales_desc + slot * (kMicroRecordBytes / 16);
+                const uint32_t to = tmem + kPieceTokens * kPieces + slot * 16;
+                copy_scales(leader, to, as);
+                copy_scales(leader, to + 8, bs);
+                copy_scales(leader, to + 4, as + 32);
+                copy_scales(leader, to + 12, bs + 32);
+                const uint32_t steps = (cols - (task.first + k) * kMicroCols + 63) / 64;
+#pragma unroll
+                for (uint32_t q = 0; q < 4; ++q) {
+                    const uint32_t h = q >> 1, pair = (q & 1) * 2;
+                    mma_scaled(q < steps ? leader : 0, tmem, a + q * 2, b + q * 2, idesc | pair << 4 | pair << 29, to + h * 4, to + 8 + h * 4,
+                               k > 0 || q > 0);
+                }
+                tcgen05_commit(leader, sh.empty + slot);
+                b += record16, bs += record16;
+                if (++slot == stages) slot = 0, phase ^= 1;
             }
+            tcgen05_commit(leader, &sh.done);
+            suspended_wait(&sh.done, i & 1, &never);   // no instruction may be under way when tensor memory is given back
         } else {
             if (begins) {
                 stage(i, digits);
@@ -221,7 +227,7 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
         meet(i);
         tcgen05_fence_after();
     }
-    if (warp == 0 && lane == 0) {   // nothing may be in flight when the CTA ends
+    if (warp == 0) {   // nothing may be in flight when the CTA ends
         for (uint32_t k = asked > stages ? asked - stages : 0; k < asked; ++k) mbar_wait_bounded(sh.full + k % stages, (k / stages) & 1);
     }
     tcgen05_fence_before();
