@@ -137,6 +137,14 @@ __device__ __forceinline__ void load_eight(const uint8_t* p, int valid, uint32_t
     for (int i = 0; i < kWords; ++i) w[i] = 0;
     if (valid <= 0) return;
     const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15u;
+    if (off == 0 && valid == 8) {
+#pragma unroll
+        for (int g = 0; g < kWords / 4; ++g) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p + 16 * g));
+            w[4 * g] = v.x, w[4 * g + 1] = v.y, w[4 * g + 2] = v.z, w[4 * g + 3] = v.w;
+        }
+        return;
+    }
     const uint8_t* base = p - off;
     const int last = int(off) + valid * kElem;   // bytes from base to the end of the elements
     uint32_t a[kWords + 4];

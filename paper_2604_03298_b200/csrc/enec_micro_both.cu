@@ -3,9 +3,9 @@
 // Lanes of the accumulator are rows of W, its columns tokens. A stage is one record's 256 columns: a record lies in memory as the
 // tensor cores want it in shared memory, so a stage is a handful of bulk copies without a tensor map, and its scales go on to
 // tensor memory as they are (tcgen05.cp). At this rate what bounds a tile is how fast L2 refills shared memory: 256 rows x 192
-// tokens take 60 KB a stage for 786 clocks of matrix instructions at the nominal rate, 76 bytes a clock; 128 x 128 would take 134.
-// So the tile is the largest whose accumulators (2 x 192 columns) leave room for three stages' scales in the 512 columns of tensor
-// memory. Where such tiles would leave SMs idle, tiles of 128 rows and of 128 or 64 tokens are taken.
+// tokens take 60 KB a stage for 786 clocks of matrix instructions (98 each, measured), 76 bytes a clock, of which L2 gave 84 at
+// most; 128 x 128 would take 134. So the tile is the largest whose accumulators (2 x 192 columns) leave room for three stages'
+// scales in the 512 columns of tensor memory, or the smaller one with which the SMs' last round is fuller.
 #include "enec_micro_mma.cuh"
 
 #include "enec_micro_launch.cuh"
@@ -14,7 +14,7 @@ namespace enec {
 namespace {
 
 constexpr uint32_t kBothStages = 3;
-constexpr uint32_t kBothThreads = 192;       // copies, matrix instructions, four warps that store
+constexpr uint32_t kBothThreads = 320;       // copies, matrix instructions, eight warps that store
 constexpr uint32_t kBothMostTokens = 192;    // of a tile
 constexpr uint32_t kScaleColumns = 32;       // of a stage in tensor memory: 8 for each 128 rows of W, 16 for the tokens
 
@@ -134,17 +134,16 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
         const bool good = micro_header_ok(job.w, job.sw) && micro_header_ok(job.x, job.sx);
         if (!suspended_wait(&done, 0, &failed)) failed = 1;
         tcgen05_fence_after();
-        const uint32_t quarter = warp & 3;   // the lanes of tensor memory that this warp may read
-        const bool wide = (job.ld_y & 1) == 0;
+        const uint32_t quarter = warp & 3, half = (warp - 2) >> 2;   // the lanes of tensor memory that this warp may read; which 16 tokens in 32
         if (good && !failed) {
             for (uint32_t i = 0; i < mt; ++i) {
                 const uint32_t row = (row_tile + i) * kMicroRows + quarter * 32 + lane;
-                for (uint32_t c = 0; c < n; c += 16) {
+                for (uint32_t c = half * 16; c < n; c += 32) {
                     if (token0 + c >= job.sx.rows) break;
                     uint32_t v[16];
                     tmem_load16(tmem + (quarter * 32 << 16) + i * kBothMostTokens + c, v);
                     tmem_load_wait();
-                    store_tile16<DT>(job.y, job.ld_y, token0 + c, job.sx.rows, row, job.sw.rows, v, 1.f, wide, lane);
+                    store_tile16<DT>(job.y, job.ld_y, token0 + c, job.sx.rows, row, job.sw.rows, v, 1.f, lane);
                 }
             }
         }
@@ -161,10 +160,9 @@ template <int DT, int MT>
 enec_status launch_both(const BothJob& job, uint32_t grid, const MicroDevice& dev, cudaStream_t stream) {
     static std::atomic<uint64_t> allowed{0};
     constexpr uint32_t most = kBothStages * both_stage_bytes<MT>(kBothMostTokens) + 1024;
-    if (!allow_shared(allowed, dev, enec_micro_both_kernel<DT, MT>, most)) return ENEC_ERR_CUDA;
-    // at least half an SM's memory and a kilobyte: two CTAs of 512 columns of tensor memory each cannot share an SM
+    if (!allow_shared(allowed, dev, enec_micro_both_kernel<DT, MT>, most < kTmemAloneShared ? kTmemAloneShared : most)) return ENEC_ERR_CUDA;
     uint32_t bytes = kBothStages * both_stage_bytes<MT>(job.tile_tokens) + 1024;
-    if (bytes < kFewHalfShared + 1024) bytes = kFewHalfShared + 1024;
+    if (bytes < kTmemAloneShared) bytes = kTmemAloneShared;
     const cudaError_t err = launch_pdl(enec_micro_both_kernel<DT, MT>, grid, kBothThreads, bytes, stream, job);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return err == cudaSuccess ? ENEC_OK : ENEC_ERR_CUDA;
@@ -192,12 +190,20 @@ extern "C" enec_status enec_matmul_microscaled_both(const void* d_x, size_t x_si
     job.y = static_cast<uint8_t*>(d_y);
     job.ld_y = ld_y;
     job.status = d_status;
-    // the largest tile with which there is work for most SMs, or the smallest
+    // the tile whose rounds over the SMs cost least: a tile's time is that of its matrix instructions or of refilling shared memory at 84
+    // bytes a clock, whichever is longer, over its records, and some 3000 clocks for filling the ring and storing. Tokens in steps of 64:
+    // a tile then begins at row 0 or 64 of a record, and its scales at an even column of tensor memory
     uint32_t mt = 2, n = kBothMostTokens;
+    uint64_t least = ~uint64_t(0);
+    for (uint32_t m = 2; m >= 1; --m) {
+        for (uint32_t k = kBothMostTokens; k >= 64; k -= 64) {
+            const uint64_t all = uint64_t((job.sw.row_tiles + m - 1) / m) * ((tokens + k - 1) / k);
+            const uint32_t instructions = 4 * m * (k > 128 ? k / 2 + 2 : 65), refill = (m * kMicroRecordBytes + k * 128 + 2048) / 84;
+            const uint64_t cost = (all + dev.sms - 1) / dev.sms * (uint64_t(job.sw.col_tiles) * (instructions > refill ? instructions : refill) + 3000);
+            if (cost < least) least = cost, mt = m, n = k;
+        }
+    }
     auto tiles = [&]() { return uint64_t((job.sw.row_tiles + mt - 1) / mt) * ((tokens + n - 1) / n); };
-    while (n > 64 && tokens <= n - 64) n -= 64;
-    if (tiles() * 4 < uint64_t(dev.sms) * 3) mt = 1;
-    while (n > 64 && tiles() * 4 < uint64_t(dev.sms) * 3) n -= 64;
     job.tile_tokens = n;
     job.row_tiles = (job.sw.row_tiles + mt - 1) / mt;
     if (tiles() >> 31) return ENEC_ERR_TOO_LARGE;

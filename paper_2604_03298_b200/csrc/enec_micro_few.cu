@@ -26,6 +26,13 @@ struct FewJob {
     int* status;
 };
 
+struct FewTasks {
+    PieceTask task;
+    uint64_t step;       // bytes from a row tile to the CTA's next one
+    __device__ __forceinline__ PieceTask get() const { return task; }
+    __device__ __forceinline__ void next() { task.records += step; }
+};
+
 template <int DT>
 __global__ void __launch_bounds__(kPieceThreads, 1) enec_micro_few_kernel(const __grid_constant__ FewJob job) {
     extern __shared__ uint8_t raw[];
@@ -37,6 +44,7 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_micro_few_kernel(const 
     const uint32_t first_tile = blockIdx.x / job.cluster, step = gridDim.x / job.cluster;
     const uint32_t n_tasks = (job.s.row_tiles - first_tile + step - 1) / step;
     const uint32_t first = min(rank * job.share, job.s.col_tiles), count = min(job.share, job.s.col_tiles - first);
+    const uint64_t tile_bytes = uint64_t(job.s.col_tiles) * kMicroRecordBytes;
     const uint32_t columns = piece_columns(job.tokens), record_bytes = piece_record_bytes(job.tokens);
     float* sums = reinterpret_cast<float*>(smem + job.stages * kMicroRecordBytes + job.share * record_bytes);   // two sets of [token][row]
     piece_setup(sh, job.stages);
@@ -46,19 +54,9 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_micro_few_kernel(const 
     const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
     piece_products(
         sh, smem, job.stages, n_tasks, job.s.cols,
-        [&](uint32_t i) {
-            return PieceTask{job.w + kMicroHeaderBytes + uint64_t(first_tile + i * step) * job.s.col_tiles * kMicroRecordBytes, first, count, 0, 0};
-        },
+        FewTasks{PieceTask{job.w + kMicroHeaderBytes + first_tile * tile_bytes, first, count, 0, 0}, step * tile_bytes},
         [&](uint32_t, uint32_t at) {
-            for (uint32_t task = worker; task < count * job.tokens; task += kPieceWorkers) {
-                const uint32_t k = task / job.tokens, token = task % job.tokens;
-                const uint32_t col = (first + k) * kMicroCols + 8 * lane;
-                uint32_t w[4];
-                load_eight<DT>(job.x + (uint64_t(token) * job.ld_x + col) * 2, col < job.s.cols ? int(min(job.s.cols - col, 8u)) : 0, w);
-                float x[8];
-                as_floats<DT>(w, x);
-                put_digits(x, token, at + k * record_bytes, columns, lane);
-            }
+            stage_rows<DT>(worker, lane, count, job.tokens, at, [&](uint32_t c) { return job.x + uint64_t(c) * job.ld_x * 2; }, first, job.s.cols);
         },
         [&](uint32_t) { return columns; },
         [&](uint32_t i, uint32_t tmem, bool ok) {
@@ -69,11 +67,8 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_micro_few_kernel(const 
                 else if (good && ok && row < job.s.rows) reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
             }
         },
+        [](uint32_t, bool) {}, job.cluster > 1,
         [&](uint32_t i) {
-            if (job.cluster == 1) {
-                __syncthreads();
-                return;
-            }
             auto cluster = cooperative_groups::this_cluster();
             cluster.sync();   // a set of sums is written again behind the next one of these, and has been read by then
             const uint32_t r = threadIdx.x & 127, row = (first_tile + i * step) * kMicroRows + r;
@@ -97,7 +92,8 @@ uint32_t few_bytes(uint32_t share, uint32_t tokens, uint32_t cluster, uint32_t& 
     if (others + 4 * kMicroRecordBytes > kFewMostShared) return 0;
     const uint64_t fit = (kFewMostShared - others) / kMicroRecordBytes;
     stages = fit < kPieceMostStages ? uint32_t(fit) : kPieceMostStages;
-    return uint32_t(others + stages * kMicroRecordBytes);
+    const uint32_t bytes = uint32_t(others + stages * kMicroRecordBytes);
+    return bytes < kTmemAloneShared ? kTmemAloneShared : bytes;
 }
 
 template <int DT>

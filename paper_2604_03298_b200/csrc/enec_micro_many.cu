@@ -286,7 +286,6 @@ __global__ void __launch_bounds__(kManyThreads, MT == 1 ? 2 : 1) enec_micro_many
         // results: the warp's quarter of the lanes, every other 16 tokens
         const uint32_t quarter = warp & 3, group = (warp - kFirstW) >> 2;
         const uint32_t row_in = quarter * 32 + lane;
-        const bool wide = (job.ld_y & 1) == 0;
         float factor[MT];
 #pragma unroll
         for (uint32_t i = 0; i < MT; ++i) factor[i] = 1.f;
@@ -315,7 +314,7 @@ __global__ void __launch_bounds__(kManyThreads, MT == 1 ? 2 : 1) enec_micro_many
 #pragma unroll
                         for (uint32_t e = 0; e < 16; ++e) sums[(c + e) * kMicroRows + row_in] = __uint_as_float(v[e]) * factor[i];
                     } else if (good) {
-                        store_tile16<DT>(job.y, job.ld_y, token0 + c, job.tokens, row, job.s.rows, v, factor[i], wide, lane);
+                        store_tile16<DT>(job.y, job.ld_y, token0 + c, job.tokens, row, job.s.rows, v, factor[i], lane);
                     }
                 }
             }
@@ -360,6 +359,8 @@ enec_status launch_many(const ManyJob& job, uint32_t tiles, const MicroDevice& d
     cfg.blockDim = dim3(kManyThreads);
     cfg.dynamicSmemBytes = many_bytes<MT>(job.tile_tokens);
     if (job.cluster > 1 && cfg.dynamicSmemBytes < job.tile_tokens * kMicroRows * 4 + 1024) cfg.dynamicSmemBytes = job.tile_tokens * kMicroRows * 4 + 1024;
+    const uint32_t least = MT * job.tile_tokens > 256 ? kTmemAloneShared : kTmemHalfShared;
+    if (cfg.dynamicSmemBytes < least) cfg.dynamicSmemBytes = least;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -1,14 +1,20 @@
 // tcgen05 in the form the products use it: one CTA per tile, accumulators in tensor memory, operands in shared memory, K-major
 // with rows of 128 bytes whose 16-byte chunks are exchanged by the row's number mod 8.
 //
-// One thread issues. The whole warp runs its loop, waits included, and the issuing instructions are predicated on the elected lane: so
-// control flow and descriptors stay uniform. With the loop inside a branch for one lane every descriptor goes through a vector
-// register first, and a record of 8 matrix and 8 copy instructions took 3800 clocks instead of 800.
+// One thread issues. The whole warp runs its loop, waits included, and the issuing instructions are predicated on the elected lane, so
+// that control flow and descriptors stay uniform: four small matrix instructions with their scales and waits take 260 clocks to
+// issue, 370 with a branch for one lane around them.
 #pragma once
 
 #include "enec_micro.cuh"
 
 namespace enec {
+
+// Dynamic shared memory that a kernel takes at least, by its columns of tensor memory: above 256, or up to 256. On an SM's 228 KB two
+// CTAs can then only be neighbours if there is room for both their columns, so no allocation ever waits for another CTA. (One that did
+// could wait forever: CTAs of two clusters, each holding columns on one SM and waiting for them on another, meet in no barrier.)
+constexpr uint32_t kTmemAloneShared = 160 * 1024;
+constexpr uint32_t kTmemHalfShared = 77 * 1024;
 
 #ifdef __CUDACC__
 
@@ -92,27 +98,26 @@ __device__ __forceinline__ void tmem_load16(uint32_t tmem, uint32_t* v) {
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Stores a warp's 32 rows (lanes) x 16 tokens (registers) to y[token][row]. Two tokens at a time, neighbouring lanes exchange values
-// so that each stores two rows of one token: 4 bytes a lane instead of 2. `wide`: y and its rows lie on 4-byte boundaries.
+// so that each stores two rows of one token: 4 bytes a lane instead of 2. Where a row of y or the matrix ends unevenly, one by one.
 template <int DT>
 __device__ __forceinline__ void store_tile16(uint8_t* y, uint64_t ld_y, uint32_t token, uint32_t tokens, uint32_t row, uint32_t rows,
-                                             const uint32_t* v, float factor, bool wide, uint32_t lane) {
+                                             const uint32_t* v, float factor, uint32_t lane) {
     using T = typename MicroType<DT>::T;
+    const uint32_t odd = lane & 1, first = row & ~1u;    // the token of two, and the first of the two rows, that this lane stores
+    T* at = reinterpret_cast<T*>(y) + uint64_t(token + odd) * ld_y + first;
+    const bool whole = (ld_y & 1) == 0 && token + 16 <= tokens && (row | 31) < rows;   // the same for the whole warp
 #pragma unroll
     for (int j = 0; j < 16; j += 2) {
         const float a = __uint_as_float(v[j]) * factor, b = __uint_as_float(v[j + 1]) * factor;
-        const float theirs = __shfl_xor_sync(0xFFFFFFFFu, lane & 1 ? a : b, 1);
-        const uint32_t to = token + j + (lane & 1);
-        const uint32_t first = row & ~1u;    // of the two rows that this lane stores
-        const float low = lane & 1 ? theirs : a, high = lane & 1 ? b : theirs;
-        if (to < tokens) {
-            T* at = reinterpret_cast<T*>(y) + uint64_t(to) * ld_y + first;
-            if (wide && first + 1 < rows) {
-                *reinterpret_cast<uint32_t*>(at) = MicroType<DT>::pack(low, high);
-            } else {
-                if (first < rows) at[0] = MicroType<DT>::one(low);
-                if (first + 1 < rows) at[1] = MicroType<DT>::one(high);
-            }
+        const float theirs = __shfl_xor_sync(0xFFFFFFFFu, odd ? a : b, 1);
+        const float low = odd ? theirs : a, high = odd ? b : theirs;
+        if (whole) {
+            *reinterpret_cast<uint32_t*>(at) = MicroType<DT>::pack(low, high);
+        } else if (token + j + odd < tokens) {
+            if (first < rows) at[0] = MicroType<DT>::one(low);
+            if (first + 1 < rows) at[1] = MicroType<DT>::one(high);
         }
+        at += 2 * ld_y;
     }
 }
 

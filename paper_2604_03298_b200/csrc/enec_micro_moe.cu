@@ -54,64 +54,70 @@ struct MoeJob {
 
 // Shared memory: [routing tables | ring | digits]; the router's sums use what lies behind the tables.
 __host__ __device__ inline uint32_t routing_bytes(uint32_t pairs, uint32_t experts) {
-    return (pairs * 8 + (3 * experts + 4) * 2 + 1023) / 1024 * 1024;
+    return (pairs * 8 + (experts + 1) * 10 + 1023) / 1024 * 1024;
 }
 struct Routing {
     float* weight;            // [pairs]
     uint16_t* expert;         // [pairs]
     uint16_t* list;           // [pairs]: pairs by expert, then by number
-    uint16_t* count;          // [experts]
+    uint32_t* count;          // [experts + 1]
     uint16_t* first;          // [experts + 1]: into list
+    uint16_t* next;           // [experts + 1]
     uint16_t* group_first;    // [experts + 1]
     uint32_t pairs, experts;
 };
 __device__ __forceinline__ Routing routing_at(uint8_t* smem, uint32_t pairs, uint32_t experts) {
     Routing r;
     r.weight = reinterpret_cast<float*>(smem);
-    r.expert = reinterpret_cast<uint16_t*>(r.weight + pairs);
+    r.count = reinterpret_cast<uint32_t*>(r.weight + pairs);
+    r.expert = reinterpret_cast<uint16_t*>(r.count + experts + 1);
     r.list = r.expert + pairs;
-    r.count = r.list + pairs;
-    r.first = r.count + experts;
-    r.group_first = r.first + experts + 1;
+    r.first = r.list + pairs;
+    r.next = r.first + experts + 1;
+    r.group_first = r.next + experts + 1;
     r.pairs = pairs;
     r.experts = experts;
     return r;
 }
 
-// From every pair's expert: the pairs of each expert in order, cut into groups. Called by the whole CTA.
+// From every pair's expert: the pairs of each expert in order, cut into groups. Called by the whole CTA; every CTA of both launches has
+// to come to the same groups, so a pair's place goes by its number, not by which thread was faster.
 __device__ __forceinline__ void build_lists(const Routing& r, uint32_t group) {
-    for (uint32_t e = threadIdx.x; e < r.experts; e += blockDim.x) {
-        uint32_t n = 0;
-        for (uint32_t p = 0; p < r.pairs; ++p) n += r.expert[p] == e;
-        r.count[e] = uint16_t(n);
-    }
+    for (uint32_t e = threadIdx.x; e <= r.experts; e += blockDim.x) r.count[e] = 0;
+    __syncthreads();
+    for (uint32_t p = threadIdx.x; p < r.pairs; p += blockDim.x) atomicAdd(r.count + r.expert[p], 1u);
     __syncthreads();
     if (threadIdx.x < 32) {
+        const uint32_t lane = threadIdx.x;
         uint32_t pairs = 0, groups = 0;
         for (uint32_t e0 = 0; e0 < r.experts; e0 += 32) {
-            const uint32_t e = e0 + threadIdx.x;
+            const uint32_t e = e0 + lane;
             const uint32_t n = e < r.experts ? r.count[e] : 0, g = (n + group - 1) / group;
             uint32_t sum_n = n, sum_g = g;
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
                 const uint32_t a = __shfl_up_sync(0xFFFFFFFFu, sum_n, d), b = __shfl_up_sync(0xFFFFFFFFu, sum_g, d);
-                if (int(threadIdx.x) >= d) sum_n += a, sum_g += b;
+                if (int(lane) >= d) sum_n += a, sum_g += b;
             }
             if (e < r.experts) {
                 r.first[e] = uint16_t(pairs + sum_n - n);
+                r.next[e] = uint16_t(pairs + sum_n - n);
                 r.group_first[e] = uint16_t(groups + sum_g - g);
             }
             pairs += __shfl_sync(0xFFFFFFFFu, sum_n, 31);
             groups += __shfl_sync(0xFFFFFFFFu, sum_g, 31);
         }
-        if (threadIdx.x == 0) r.first[r.experts] = uint16_t(pairs), r.group_first[r.experts] = uint16_t(groups);
-    }
-    __syncthreads();
-    for (uint32_t e = threadIdx.x; e < r.experts; e += blockDim.x) {
-        if (r.count[e] == 0) continue;
-        uint32_t at = r.first[e];
-        for (uint32_t p = 0; p < r.pairs; ++p)
-            if (r.expert[p] == e) r.list[at++] = uint16_t(p);
+        if (lane == 0) r.first[r.experts] = uint16_t(pairs), r.group_first[r.experts] = uint16_t(groups);
+        __syncwarp();
+        for (uint32_t p0 = 0; p0 < r.pairs; p0 += 32) {
+            const uint32_t p = p0 + lane, e = p < r.pairs ? r.expert[p] : 0xFFFFu;
+            const uint32_t same = __match_any_sync(0xFFFFFFFFu, e);
+            const uint32_t before = __popc(same & ((1u << lane) - 1));
+            if (p < r.pairs) r.list[r.next[e] + before] = uint16_t(p);
+            __syncwarp();
+            if (p < r.pairs && before == 0) r.next[e] += uint16_t(__popc(same));
+            __syncwarp();
+        }
     }
     __syncthreads();
 }
@@ -130,7 +136,7 @@ __device__ __forceinline__ Group group_of(const Routing& r, uint32_t index, uint
     g.expert = low;
     const uint32_t begin = (index - r.group_first[low]) * group;
     g.first = r.first[low] + begin;
-    g.n = min(group, uint32_t(r.count[low]) - begin);
+    g.n = min(group, r.count[low] - begin);
     return g;
 }
 
@@ -157,37 +163,68 @@ __device__ __forceinline__ uint32_t logit_key(float v) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+// Parts of a CTA's columns that warps share in the router's products; and the bytes of its sums.
+__host__ __device__ inline uint32_t router_splits(uint32_t tokens, uint32_t experts) {
+    const uint32_t tiles = (experts + 15) / 16 * ((tokens + 7) / 8);
+    return tiles >= 16 ? 1 : 16 / tiles;
+}
+__host__ __device__ inline uint32_t router_bytes(uint32_t tokens, uint32_t experts) {
+    return (1 + router_splits(tokens, experts)) * tokens * experts * 4;
+}
+
 // The router: logits of all tokens to every CTA of the cluster, then every warp chooses for its tokens.
 template <int DT>
 __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float* scratch) {
     auto cluster = cooperative_groups::this_cluster();
     const uint32_t rank = cluster.block_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const uint32_t total = job.tokens * job.experts;
-    float* part = scratch;
-    float* logits = scratch + total;
     const uint32_t blocks = (job.hidden + 31) / 32, share = (blocks + kMoeCluster - 1) / kMoeCluster;
     const uint32_t b0 = min(rank * share, blocks), b1 = min(b0 + share, blocks);
-    const uint32_t expert_tiles = (job.experts + 15) / 16, token_tiles = (job.tokens + 7) / 8;
-    for (uint32_t unit = warp; unit < expert_tiles * token_tiles; unit += kMoeWarps) {
-        const uint32_t e = unit % expert_tiles * 16 + g, token = unit / expert_tiles * 8 + g;
-        const uint8_t* r0 = job.router + uint64_t(e) * job.hidden * 2;
-        const uint8_t* r1 = r0 + uint64_t(8) * job.hidden * 2;
-        const uint8_t* xr = job.x + uint64_t(token) * job.ld_x * 2;
+    const uint32_t expert_tiles = (job.experts + 15) / 16, token_tiles = (job.tokens + 7) / 8, tiles = expert_tiles * token_tiles;
+    // where tiles are few, warps share a tile's columns too
+    const uint32_t splits = router_splits(job.tokens, job.experts), split_blocks = (share + splits - 1) / splits;
+    float* logits = scratch;
+    float* part = scratch + total;   // [split][token][expert]
+    const bool whole = job.hidden % 32 == 0 && job.ld_x % 8 == 0;   // every load is of 16 aligned bytes
+    for (uint32_t unit = warp; unit < tiles * splits; unit += kMoeWarps) {
+        const uint32_t tile = unit % tiles, split = unit / tiles;
+        const uint32_t e = tile % expert_tiles * 16 + g, token = tile / expert_tiles * 8 + g;
+        // rows that do not exist are read from the last one's place and not written
+        const uint8_t* r0 = job.router + uint64_t(min(e, job.experts - 1)) * job.hidden * 2;
+        const uint8_t* r1 = job.router + uint64_t(min(e + 8, job.experts - 1)) * job.hidden * 2;
+        const uint8_t* xr = job.x + uint64_t(min(token, job.tokens - 1)) * job.ld_x * 2;
+        const uint32_t first = min(b0 + split * split_blocks, b1), last = min(first + split_blocks, b1);
         float c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (uint32_t b = b0; b < b1; ++b) {
-            const uint32_t col = 32 * b + 8 * t;
-            const int valid = col < job.hidden ? int(min(job.hidden - col, 8u)) : 0;
-            uint32_t a0[4], a1[4], bx[4];
-            load_eight<DT>(r0 + uint64_t(col) * 2, e < job.experts ? valid : 0, a0);
-            load_eight<DT>(r1 + uint64_t(col) * 2, e + 8 < job.experts ? valid : 0, a1);
-            load_eight<DT>(xr + uint64_t(col) * 2, token < job.tokens ? valid : 0, bx);
-            mma_native<DT>(c, a0, a1, bx);
+        constexpr uint32_t kBatch = 4;
+        for (uint32_t b = first; b < last; b += kBatch) {
+            uint32_t a0[kBatch][4], a1[kBatch][4], bx[kBatch][4];
+            if (whole && b + kBatch <= last) {
+#pragma unroll
+                for (uint32_t i = 0; i < kBatch; ++i) {
+                    const uint64_t at = uint64_t(32 * (b + i) + 8 * t) * 2;
+                    const uint4 v0 = __ldg(reinterpret_cast<const uint4*>(r0 + at)), v1 = __ldg(reinterpret_cast<const uint4*>(r1 + at)),
+                                v2 = __ldg(reinterpret_cast<const uint4*>(xr + at));
+                    a0[i][0] = v0.x, a0[i][1] = v0.y, a0[i][2] = v0.z, a0[i][3] = v0.w;
+                    a1[i][0] = v1.x, a1[i][1] = v1.y, a1[i][2] = v1.z, a1[i][3] = v1.w;
+                    bx[i][0] = v2.x, bx[i][1] = v2.y, bx[i][2] = v2.z, bx[i][3] = v2.w;
+                }
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < kBatch; ++i) {
+                    const uint32_t col = 32 * (b + i) + 8 * t;
+                    const int valid = b + i < last && col < job.hidden ? int(min(job.hidden - col, 8u)) : 0;
+                    load_eight<DT>(r0 + uint64_t(col) * 2, valid, a0[i]);
+                    load_eight<DT>(r1 + uint64_t(col) * 2, valid, a1[i]);
+                    load_eight<DT>(xr + uint64_t(col) * 2, valid, bx[i]);
+                }
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < kBatch; ++i) mma_native<DT>(c, a0[i], a1[i], bx[i]);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t ee = unit % expert_tiles * 16 + g + (i >> 1) * 8, tt = unit / expert_tiles * 8 + 2 * t + (i & 1);
-            if (ee < job.experts && tt < job.tokens) part[tt * job.experts + ee] = c[i];
+            const uint32_t ee = tile % expert_tiles * 16 + g + (i >> 1) * 8, tt = tile / expert_tiles * 8 + 2 * t + (i & 1);
+            if (ee < job.experts && tt < job.tokens) part[split * total + tt * job.experts + ee] = c[i];
         }
     }
     cluster.sync();
@@ -195,7 +232,10 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
     for (uint32_t i = rank * per + threadIdx.x; i < min(total, (rank + 1) * per); i += blockDim.x) {
         float v = 0.f;
 #pragma unroll
-        for (uint32_t k = 0; k < kMoeCluster; ++k) v += cluster.map_shared_rank(part, k)[i];
+        for (uint32_t k = 0; k < kMoeCluster; ++k) {
+            const float* theirs = cluster.map_shared_rank(part, k);
+            for (uint32_t s = 0; s < splits; ++s) v += theirs[s * total + i];
+        }
 #pragma unroll
         for (uint32_t k = 0; k < kMoeCluster; ++k) cluster.map_shared_rank(logits, k)[i] = v;
     }
@@ -249,24 +289,45 @@ __device__ __forceinline__ uint32_t choose_slices(uint64_t tasks, uint32_t recor
 struct Tasks {
     uint32_t matrices, tiles, slices, records, share;
     uint32_t begin, end;
-    struct Which {
-        uint32_t group, matrix, tile, slice;
-    };
     __device__ __forceinline__ Tasks(uint32_t groups, uint32_t matrices_, const MicroShape& s, uint32_t slices_)
         : matrices(matrices_), tiles(s.row_tiles), slices(slices_), records(s.col_tiles), share((s.col_tiles + slices_ - 1) / slices_) {
         const uint64_t all = uint64_t(groups) * matrices * tiles * slices;
         begin = uint32_t(all * blockIdx.x / gridDim.x);
         end = uint32_t(all * (blockIdx.x + 1) / gridDim.x);
     }
-    __device__ __forceinline__ Which which(uint32_t i) const {
-        const uint32_t t = begin + i;
-        return {t / (slices * tiles * matrices), t / (slices * tiles) % matrices, t / slices % tiles, t % slices};
+};
+// A walk over a CTA's tasks: divisions once, then counting.
+struct Walk {
+    const Tasks& tasks;
+    const Routing& r;
+    uint32_t group_size;
+    const uint8_t* m0;
+    const uint8_t* m1;
+    uint32_t group, matrix, tile, slice;
+    Group now;
+    __device__ __forceinline__ Walk(const Tasks& tasks_, const Routing& r_, uint32_t group_size_, const uint8_t* m0_, const uint8_t* m1_)
+        : tasks(tasks_), r(r_), group_size(group_size_), m0(m0_), m1(m1_) {
+        slice = tasks.begin % tasks.slices;
+        const uint32_t rest = tasks.begin / tasks.slices;
+        tile = rest % tasks.tiles;
+        matrix = rest / tasks.tiles % tasks.matrices;
+        group = rest / tasks.tiles / tasks.matrices;
+        if (tasks.begin < tasks.end) now = group_of(r, group, group_size);
     }
-    __device__ __forceinline__ PieceTask task(const Routing& r, uint32_t i, uint32_t group, const uint8_t* m0, const uint8_t* m1) const {
-        const Which w = which(i);
-        const uint64_t tile = uint64_t(group_of(r, w.group, group).expert) * tiles + w.tile;
-        const uint32_t first = min(w.slice * share, records);
-        return {(w.matrix ? m1 : m0) + kMicroHeaderBytes + tile * records * kMicroRecordBytes, first, min(share, records - first), w.group, first};
+    __device__ __forceinline__ PieceTask get() const {
+        const uint32_t first = min(slice * tasks.share, tasks.records);
+        const uint64_t strip = uint64_t(now.expert) * tasks.tiles + tile;
+        return {(matrix ? m1 : m0) + kMicroHeaderBytes + strip * tasks.records * kMicroRecordBytes, first, min(tasks.share, tasks.records - first), group,
+                first};
+    }
+    __device__ __forceinline__ void next() {
+        if (++slice < tasks.slices) return;
+        slice = 0;
+        if (++tile < tasks.tiles) return;
+        tile = 0;
+        if (++matrix < tasks.matrices) return;
+        matrix = 0;
+        if (++group < r.group_first[r.experts]) now = group_of(r, group, group_size);
     }
 };
 
@@ -294,36 +355,25 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_in_kernel(const __g
     }
     const bool good = micro_header_ok(job.gate, job.s_in) && micro_header_ok(job.up, job.s_in);
     const Tasks tasks(groups, 2, job.s_in, slices);
-    Group now = {};
     const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
+    Walk walk(tasks, r, job.group, job.gate, job.up), here = walk;
     piece_products(
-        sh, smem + tables, job.stages, tasks.end - tasks.begin, job.hidden,
-        [&](uint32_t i) { return tasks.task(r, i, job.group, job.gate, job.up); },
-        [&](uint32_t i, uint32_t at) {
-            now = group_of(r, tasks.which(i).group, job.group);
-            const uint32_t columns = piece_columns(now.n), record_bytes = piece_record_bytes(now.n);
-            for (uint32_t task = worker; task < tasks.records * now.n; task += kPieceWorkers) {
-                const uint32_t k = task / now.n, c = task % now.n;
-                const uint32_t col = k * kMicroCols + 8 * lane;
-                uint32_t w[4];
-                load_eight<DT>(job.x + (uint64_t(r.list[now.first + c] / job.top) * job.ld_x + col) * 2,
-                               col < job.hidden ? int(min(job.hidden - col, 8u)) : 0, w);
-                float x[8];
-                as_floats<DT>(w, x);
-                put_digits(x, c, at + k * record_bytes, columns, lane);
-            }
+        sh, smem + tables, job.stages, tasks.end - tasks.begin, job.hidden, walk,
+        [&](uint32_t, uint32_t at) {
+            stage_rows<DT>(worker, lane, tasks.records, here.now.n, at,
+                           [&](uint32_t c) { return job.x + uint64_t(r.list[here.now.first + c] / job.top) * job.ld_x * 2; }, 0, job.hidden);
         },
         [&](uint32_t group) { return piece_columns(group_of(r, group, job.group).n); },
-        [&](uint32_t i, uint32_t tmem, bool ok) {
-            const Tasks::Which w = tasks.which(i);
-            const uint32_t row = w.tile * kMicroRows + row_in;
-            const bool any = w.slice * tasks.share < tasks.records;
-            for (uint32_t c = worker >> 2; c < now.n; c += kPieceWorkers / 4) {
+        [&](uint32_t, uint32_t tmem, bool ok) {
+            const uint32_t row = here.tile * kMicroRows + row_in;
+            const bool any = here.slice * tasks.share < tasks.records;
+            for (uint32_t c = worker >> 2; c < here.now.n; c += kPieceWorkers / 4) {
                 const float v = any ? take_sum(tmem, c) : 0.f;
-                if (good && ok && row < job.inter) job.in_sums[(uint64_t(w.slice * 2 + w.matrix) * pairs + r.list[now.first + c]) * job.ld_h + row] = v;
+                if (good && ok && row < job.inter)
+                    job.in_sums[(uint64_t(here.slice * 2 + here.matrix) * pairs + r.list[here.now.first + c]) * job.ld_h + row] = v;
             }
         },
-        [&](uint32_t) { __syncthreads(); });
+        [&](uint32_t, bool) { here.next(); }, false, [](uint32_t) {});
     if (threadIdx.x == 0) {
         if (sh.failed) report(job.status, ENEC_ERR_TIMEOUT);
         else if (!good && blockIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
@@ -351,21 +401,19 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_out_kernel(const __
     const uint32_t groups = r.group_first[job.experts];
     const uint32_t slices = choose_slices(uint64_t(groups) * job.s_out.row_tiles, job.s_out.col_tiles, job.most_slices);
     const Tasks tasks(groups, 1, job.s_out, slices);
-    Group now = {};
     const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
+    Walk walk(tasks, r, job.group, job.down, nullptr), here = walk;
     piece_products(
-        sh, smem + tables, job.stages, tasks.end - tasks.begin, job.inter,
-        [&](uint32_t i) { return tasks.task(r, i, job.group, job.down, nullptr); },
-        [&](uint32_t i, uint32_t at) {
-            now = group_of(r, tasks.which(i).group, job.group);
-            const uint32_t columns = piece_columns(now.n), record_bytes = piece_record_bytes(now.n);
-            for (uint32_t task = worker; task < tasks.records * now.n; task += kPieceWorkers) {
-                const uint32_t k = task / now.n, c = task % now.n;
+        sh, smem + tables, job.stages, tasks.end - tasks.begin, job.inter, walk,
+        [&](uint32_t, uint32_t at) {
+            const uint32_t n = here.now.n, columns = piece_columns(n), record_bytes = piece_record_bytes(n);
+            for (uint32_t task = worker; task < tasks.records * n; task += kPieceWorkers) {
+                const uint32_t k = task / n, c = task % n;
                 const uint32_t col = k * kMicroCols + 8 * lane;
                 const int valid = col < job.inter ? int(min(job.inter - col, 8u)) : 0;
                 float a[8] = {}, u[8] = {};
                 for (uint32_t s = 0; s < in_slices; ++s) {
-                    const float* from = job.in_sums + (uint64_t(s * 2) * pairs + r.list[now.first + c]) * job.ld_h + col;
+                    const float* from = job.in_sums + (uint64_t(s * 2) * pairs + r.list[here.now.first + c]) * job.ld_h + col;
                     uint32_t wa[8], wu[8];
                     load_eight<ENEC_FP32>(reinterpret_cast<const uint8_t*>(from), valid, wa);
                     load_eight<ENEC_FP32>(reinterpret_cast<const uint8_t*>(from + uint64_t(pairs) * job.ld_h), valid, wu);
@@ -378,19 +426,22 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_out_kernel(const __
             }
         },
         [&](uint32_t group) { return piece_columns(group_of(r, group, job.group).n); },
-        [&](uint32_t i, uint32_t tmem, bool ok) {
-            const Tasks::Which w = tasks.which(i);
-            const uint32_t row = w.tile * kMicroRows + row_in;
-            const bool any = w.slice * tasks.share < tasks.records;
-            for (uint32_t c = worker >> 2; c < now.n; c += kPieceWorkers / 4) {
+        [&](uint32_t, uint32_t tmem, bool) {
+            const uint32_t row = here.tile * kMicroRows + row_in;
+            const bool any = here.slice * tasks.share < tasks.records;
+            for (uint32_t c = worker >> 2; c < here.now.n; c += kPieceWorkers / 4) {
                 const float v = any ? take_sum(tmem, c) : 0.f;
-                const uint32_t pair = r.list[now.first + c];
-                if (row < job.hidden) __stcg(job.out_sums + (uint64_t(w.slice) * pairs + pair) * job.hidden + row, v * r.weight[pair]);
+                const uint32_t pair = r.list[here.now.first + c];
+                if (row < job.hidden) __stcg(job.out_sums + (uint64_t(here.slice) * pairs + pair) * job.hidden + row, v * r.weight[pair]);
             }
+        },
+        [&](uint32_t, bool ok) {
+            const uint32_t tile = here.tile, row = tile * kMicroRows + row_in;
+            here.next();
             // every worker's values are visible to all before the ticket counts the task
             __threadfence();
             asm volatile("bar.sync 1, %0;" ::"n"(kPieceWorkers * 32) : "memory");
-            if (worker == 0 && lane == 0) last = atomicAdd(job.tickets + w.tile, 1u) == groups * slices - 1;
+            if (worker == 0 && lane == 0) last = atomicAdd(job.tickets + tile, 1u) == groups * slices - 1;
             asm volatile("bar.sync 1, %0;" ::"n"(kPieceWorkers * 32) : "memory");
             if (!last || !good || !ok) return;
             __threadfence();
@@ -403,7 +454,7 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_out_kernel(const __
                 reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
             }
         },
-        [&](uint32_t) { __syncthreads(); });
+        false, [](uint32_t) {});
     if (threadIdx.x == 0) {
         if (sh.failed) report(job.status, ENEC_ERR_TIMEOUT);
         else if (!good && blockIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
@@ -419,6 +470,7 @@ bool choose_group(uint32_t fixed, uint32_t records, uint32_t most, uint32_t leas
         stages = fit < kPieceMostStages ? uint32_t(fit) : kPieceMostStages;
         bytes = uint32_t(others + stages * kMicroRecordBytes);
         if (bytes < 1024 + fixed + least_bytes) bytes = 1024 + fixed + least_bytes;
+        if (bytes < kTmemAloneShared) bytes = kTmemAloneShared;
         return bytes <= kFewMostShared;
     }
     return false;
@@ -459,7 +511,7 @@ enec_status launch_moe(MoeJob job, const MicroDevice& dev, cudaStream_t stream) 
     static std::atomic<uint64_t> allowed_in{0}, allowed_out{0};
     MoeJob second = job;
     uint32_t bytes2 = 0;
-    if (!choose_group(tables, job.s_in.col_tiles, most, 8 * job.tokens * job.experts, job.group, job.stages, bytes) ||
+    if (!choose_group(tables, job.s_in.col_tiles, most, router_bytes(job.tokens, job.experts), job.group, job.stages, bytes) ||
         !choose_group(tables, job.s_out.col_tiles, most, 0, second.group, second.stages, bytes2))
         return ENEC_ERR_TOO_LARGE;
     if (!allow_shared(allowed_in, dev, enec_moe_in_kernel<DT>, kFewMostShared) ||

@@ -14,8 +14,9 @@
 // What x loses: it is rounded to 2^-22 of the largest of its 32 neighbours (all bits of a bf16 value down to 2^-14 of the largest, of an
 // fp16 value down to 2^-11). A NaN or an infinity makes its column NaN.
 //
-// A CTA takes tasks: 128 rows (a row tile of a matrix) x a range of records of columns. One warp copies records in bulk into a ring and
-// goes on to the next tasks' while results are taken; one issues the matrix instructions; sixteen make the digits and take results.
+// A CTA takes tasks: 128 rows (a row tile of a matrix) x a range of records of columns. One warp copies records in bulk into a ring, as
+// far ahead as the ring is long; one issues the matrix instructions, with two sets of sums in turn; sixteen make the digits and take
+// the results of one task while the next one's products run.
 #pragma once
 
 #include "enec_micro_mma.cuh"
@@ -27,7 +28,7 @@ constexpr uint32_t kPieceTokens = 16;        // columns of x that a CTA takes: 1
 constexpr uint32_t kPieceMostStages = 8;
 constexpr uint32_t kPieceWorkers = 16;       // warps
 constexpr uint32_t kPieceThreads = (2 + kPieceWorkers) * 32;
-constexpr uint32_t kPieceTmem = 256;         // columns: 128 of sums, 16 of scales for each stage
+constexpr uint32_t kPieceTmem = 512;         // columns: two sets of 128 sums, 16 of scales for each stage
 
 __host__ __device__ constexpr uint32_t piece_columns(uint32_t tokens) { return (tokens * kPieces + 15) / 16 * 16; }
 // A record's digits: rows of 128 bytes as a matrix operand, and 1024 bytes of scales.
@@ -36,7 +37,7 @@ __host__ __device__ constexpr uint32_t piece_record_bytes(uint32_t tokens) { ret
 #ifdef __CUDACC__
 
 struct PieceShared {
-    uint64_t full[kPieceMostStages], empty[kPieceMostStages], staged, done;
+    uint64_t full[kPieceMostStages], empty[kPieceMostStages], staged, done[2], drained[2];
     uint32_t tmem;
     volatile int failed;
 };
@@ -53,7 +54,7 @@ __device__ __forceinline__ void piece_setup(PieceShared& sh, uint32_t stages) {
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < stages; ++i) mbar_init(sh.full + i, 1), mbar_init(sh.empty + i, 1);
         mbar_init(&sh.staged, kPieceWorkers * 32);
-        mbar_init(&sh.done, 1);
+        for (uint32_t i = 0; i < 2; ++i) mbar_init(sh.done + i, 1), mbar_init(sh.drained + i, kPieceWorkers * 32);
         mbar_fence_init();
         sh.failed = 0;
     }
@@ -126,6 +127,31 @@ __device__ __forceinline__ void put_digits(const float* x, uint32_t column, uint
     }
 }
 
+// The workers' part of staging `n` columns over `count` records from `first` on: column c's values (16 bits) are row_of(c)'s, zeros behind
+// `cols`. Two at a time: their loads are on the way together.
+template <int DT, class RowOf>
+__device__ __forceinline__ void stage_rows(uint32_t worker, uint32_t lane, uint32_t count, uint32_t n, uint32_t at, RowOf row_of, uint32_t first,
+                                           uint32_t cols) {
+    const uint32_t columns = piece_columns(n), record_bytes = piece_record_bytes(n), total = count * n;
+    for (uint32_t task = worker; task < total; task += 2 * kPieceWorkers) {
+        uint32_t w[2][4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t here = task + j * kPieceWorkers;
+            const uint32_t col = (first + here / n) * kMicroCols + 8 * lane;
+            load_eight<DT>(here < total ? row_of(here % n) + uint64_t(col) * 2 : nullptr, here < total && col < cols ? int(min(cols - col, 8u)) : 0, w[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t here = task + j * kPieceWorkers;
+            if (here >= total) break;
+            float x[8];
+            as_floats<DT>(w[j], x);
+            put_digits(x, here % n, at + here / n * record_bytes, columns, lane);
+        }
+    }
+}
+
 // The sum of a column's eight digits for this lane's row.
 __device__ __forceinline__ float take_sum(uint32_t tmem, uint32_t column) {
     uint32_t v[8];
@@ -139,53 +165,54 @@ __device__ __forceinline__ float take_sum(uint32_t tmem, uint32_t column) {
     return sum;
 }
 
-// All roles of a CTA over its tasks. task_of(i): the i-th. stage(i, at): called by the workers' warps where a group begins, writes the
-// digits of its records to `at` on. columns_of(group): columns of the accumulator it has, a multiple of 16. finish(i, tmem, ok): by the
-// workers, takes the sums from their lanes of tensor memory; where not ok, a wait has run out and they are nothing. meet(i): where all threads meet behind every task. smem: the ring, then the
-// digits. cols: of the matrices. sh.failed is set where a wait ran out.
-template <class TaskOf, class Stage, class ColumnsOf, class Finish, class Meet>
-__device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, uint32_t stages, uint32_t n_tasks, uint32_t cols, TaskOf task_of,
-                                               Stage stage, ColumnsOf columns_of, Finish finish, Meet meet) {
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+// All roles of a CTA over its tasks. tasks: where the first one is, with get() and next(); every role walks a copy. stage(i, at): called by
+// the workers' warps where a group begins, writes the digits of its records to `at` on. columns_of(group): columns of the accumulator it
+// has, a multiple of 16. take(i, tmem, ok): by the workers, takes the sums from their lanes of tensor memory; where not ok, a wait
+// has run out and they are nothing. after(i, ok): by the workers, once the sums' place is free again. meet(i): by all threads behind
+// every task where `lockstep`. smem: the ring, then the digits. cols: of the matrices.
+template <class Tasks, class Stage, class ColumnsOf, class Take, class After, class Meet>
+__device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, uint32_t stages, uint32_t n_tasks, uint32_t cols, Tasks tasks,
+                                               Stage stage, ColumnsOf columns_of, Take take, After after, bool lockstep, Meet meet) {
+    const uint32_t warp = threadIdx.x >> 5;
     const uint32_t ring = smem_u32(smem), digits = ring + stages * kMicroRecordBytes;
     const uint32_t tmem = sh.tmem;
-    uint32_t group = 0xFFFFFFFFu, groups = 0, columns = 0;
-    uint32_t used = 0;                                                  // records of the tasks so far
-    uint32_t ask_task = 0, ask_record = 0, asked = 0, ask_slot = 0, ask_phase = 0;   // the copying warp's
-    PieceTask asking = n_tasks ? task_of(0) : PieceTask{};
-    uint32_t slot = 0, phase = 0;                                       // of the record that the matrix instructions take next
     const uint32_t leader = elected();
-    const uint64_t ring_desc = operand_desc(ring), ring_scales_desc = scale_desc(ring + kMicroElemBytes);
-    const uint64_t digits_desc = operand_desc(digits), digit_scales_desc = scale_desc(digits);
-    volatile int never = 0;
-    for (uint32_t i = 0; i < n_tasks; ++i) {
-        const PieceTask task = task_of(i);
-        const bool begins = task.group != group;
-        if (begins) group = task.group, ++groups, columns = columns_of(group);
-        const uint32_t after = used + task.count;
-        if (warp == 0) {
-            // all of this task's records, and of the next ones' as many as the ring takes once these are used
-            while (ask_task < n_tasks && asked < after + stages && !sh.failed) {
-                if (ask_record >= asking.count) {
-                    if (++ask_task < n_tasks) asking = task_of(ask_task);
-                    ask_record = 0;
-                    continue;
-                }
-                if (asked >= stages && !suspended_wait(sh.empty + ask_slot, ask_phase ^ 1, &sh.failed)) {
+    if (warp == 0) {
+        uint32_t asked = 0, slot = 0, phase = 0;
+        for (uint32_t i = 0; i < n_tasks; ++i, tasks.next()) {
+            const PieceTask task = tasks.get();
+            for (uint32_t k = 0; k < task.count && !sh.failed; ++k) {
+                if (asked >= stages && !suspended_wait(sh.empty + slot, phase ^ 1, &sh.failed)) {
                     sh.failed = 1;
                     break;
                 }
                 if (leader) {
-                    mbar_expect_tx(sh.full + ask_slot, kMicroRecordBytes);
-                    bulk_g2s(smem + ask_slot * kMicroRecordBytes, asking.records + uint64_t(asking.first + ask_record) * kMicroRecordBytes,
-                             kMicroRecordBytes, sh.full + ask_slot);
+                    mbar_expect_tx(sh.full + slot, kMicroRecordBytes);
+                    bulk_g2s(smem + slot * kMicroRecordBytes, task.records + uint64_t(task.first + k) * kMicroRecordBytes, kMicroRecordBytes,
+                             sh.full + slot);
                 }
-                ++asked, ++ask_record;
-                if (++ask_slot == stages) ask_slot = 0, ask_phase ^= 1;
+                ++asked;
+                if (++slot == stages) slot = 0, phase ^= 1;
             }
-        } else if (warp == 1) {
+            if (lockstep) meet(i);
+        }
+        // nothing may be in flight when the CTA ends
+        for (uint32_t k = asked > stages ? asked - stages : 0; k < asked; ++k) mbar_wait_bounded(sh.full + k % stages, (k / stages) & 1);
+    } else if (warp == 1) {
+        const uint64_t ring_desc = operand_desc(ring), ring_scales_desc = scale_desc(ring + kMicroElemBytes);
+        const uint64_t digits_desc = operand_desc(digits), digit_scales_desc = scale_desc(digits);
+        uint32_t group = 0xFFFFFFFFu, groups = 0, columns = 0, slot = 0, phase = 0;
+        volatile int never = 0;
+        for (uint32_t i = 0; i < n_tasks; ++i, tasks.next()) {
+            const PieceTask task = tasks.get();
+            if (task.group != group) {
+                group = task.group, columns = columns_of(group);
+                if (!suspended_wait(&sh.staged, groups++ & 1, &sh.failed)) sh.failed = 1;
+            }
+            const uint32_t set = i & 1, sums = tmem + set * (kPieceTokens * kPieces);
+            if (i >= 2 && !suspended_wait(sh.drained + set, ((i >> 1) - 1) & 1, &sh.failed)) sh.failed = 1;
+            tcgen05_fence_after();
             const uint32_t idesc = scaled_idesc(columns), record16 = columns * 8 + 64;   // a record's digits in units of 16 bytes
-            if (begins && !suspended_wait(&sh.staged, (groups - 1) & 1, &sh.failed)) sh.failed = 1;
             uint64_t b = digits_desc + task.digits * record16, bs = digit_scales_desc + columns * 8 + task.digits * record16;
             for (uint32_t k = 0; k < task.count && !sh.failed; ++k) {
                 if (!suspended_wait(sh.full + slot, phase, &sh.failed)) {
@@ -194,7 +221,7 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
                 }
                 tcgen05_fence_after();
                 const uint64_t a = ring_desc + slot * (kMicroRecordBytes / 16), as = ring_scales_desc + slot * (kMicroRecordBytes / 16);
-                const uint32_t to = tmem + kPieceTokens * kPieces + slot * 16;
+                const uint32_t to = tmem + 2 * kPieceTokens * kPieces + slot * 16;
                 copy_scales(leader, to, as);
                 copy_scales(leader, to + 8, bs);
                 copy_scales(leader, to + 4, as + 32);
@@ -203,32 +230,38 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
 #pragma unroll
                 for (uint32_t q = 0; q < 4; ++q) {
                     const uint32_t h = q >> 1, pair = (q & 1) * 2;
-                    mma_scaled(q < steps ? leader : 0, tmem, a + q * 2, b + q * 2, idesc | pair << 4 | pair << 29, to + h * 4, to + 8 + h * 4,
+                    mma_scaled(q < steps ? leader : 0, sums, a + q * 2, b + q * 2, idesc | pair << 4 | pair << 29, to + h * 4, to + 8 + h * 4,
                                k > 0 || q > 0);
                 }
                 tcgen05_commit(leader, sh.empty + slot);
                 b += record16, bs += record16;
                 if (++slot == stages) slot = 0, phase ^= 1;
             }
-            tcgen05_commit(leader, &sh.done);
-            suspended_wait(&sh.done, i & 1, &never);   // no instruction may be under way when tensor memory is given back
-        } else {
-            if (begins) {
+            tcgen05_commit(leader, sh.done + set);
+            if (lockstep) meet(i);
+        }
+        // no instruction may be under way when tensor memory is given back
+        for (uint32_t i = n_tasks > 2 ? n_tasks - 2 : 0; i < n_tasks; ++i) suspended_wait(sh.done + (i & 1), (i >> 1) & 1, &never);
+    } else {
+        uint32_t group = 0xFFFFFFFFu;
+        for (uint32_t i = 0; i < n_tasks; ++i, tasks.next()) {
+            const PieceTask task = tasks.get();
+            if (task.group != group) {
+                group = task.group;
                 stage(i, digits);
                 fence_async_shared();
                 mbar_arrive(&sh.staged);
             }
-            if (!suspended_wait(&sh.done, i & 1, &sh.failed)) sh.failed = 1;
+            const uint32_t set = i & 1;
+            if (!suspended_wait(sh.done + set, (i >> 1) & 1, &sh.failed)) sh.failed = 1;
             tcgen05_fence_after();
-            finish(i, tmem + ((warp & 3) * 32 << 16), !sh.failed);
+            const bool ok = !sh.failed;
+            take(i, tmem + set * (kPieceTokens * kPieces) + ((warp & 3) * 32 << 16), ok);
             tcgen05_fence_before();
+            mbar_arrive(sh.drained + set);
+            after(i, ok);
+            if (lockstep) meet(i);
         }
-        used = after;
-        meet(i);
-        tcgen05_fence_after();
-    }
-    if (warp == 0) {   // nothing may be in flight when the CTA ends
-        for (uint32_t k = asked > stages ? asked - stages : 0; k < asked; ++k) mbar_wait_bounded(sh.full + k % stages, (k / stages) & 1);
     }
     tcgen05_fence_before();
     __syncthreads();
