@@ -2,7 +2,7 @@
 //
 // Lanes of the accumulator are rows of W, its columns tokens: 256 (two accumulators) or 128 rows x up to 256 tokens a CTA. Of 64 columns
 // (a step) the tensor cores take 1024 clocks at 256 x 256. Meanwhile eight warps turn 16384 codes into 16-bit values in shared
-// memory (5 instructions a pair, some 370 clocks of the SM's issue slots) and four warps fetch 32 KB of x with cp.async, 32 bytes a
+// memory (5 instructions a pair, some 370 clocks of the SM's issue slots) and eight warps fetch 32 KB of x with cp.async, 32 bytes a
 // clock from L2; tiles of 128 x 256 would need twice that, more than L2 gives to all SMs at a time. Raw records are copied in bulk; a
 // thread takes its share of a record to registers at once, so that one record's room is enough.
 //
@@ -20,8 +20,8 @@
 namespace enec {
 namespace {
 
-constexpr uint32_t kManyThreads = 14 * 32;   // bulk copies, matrix instructions, 4 warps for x, 8 for the weights and the results
-constexpr uint32_t kFirstX = 2, kFirstW = 6;
+constexpr uint32_t kManyThreads = 18 * 32;   // bulk copies, matrix instructions, 8 warps for x, 8 for the weights and the results
+constexpr uint32_t kFirstX = 2, kFirstW = 10, kThreadsX = 8 * 32;
 constexpr uint32_t kStagesA = 2, kStagesB = 3;
 constexpr uint32_t kManyMostTokens = 256;
 
@@ -83,7 +83,7 @@ __device__ __forceinline__ uint4 to_fp16(uint32_t codes, uint32_t byte, uint32_t
 }
 
 template <int DT, int MT>
-__global__ void __launch_bounds__(kManyThreads, MT == 1 ? 2 : 1) enec_micro_many_kernel(const __grid_constant__ ManyJob job) {
+__global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const __grid_constant__ ManyJob job) {
     extern __shared__ uint8_t raw_shared[];
     __shared__ uint64_t raw_full, raw_empty, full_a[kStagesA], empty_a[kStagesA], full_b[kStagesB], empty_b[kStagesB], done;
     __shared__ uint32_t tmem_at;
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kManyThreads, MT == 1 ? 2 : 1) enec_micro_many
         mbar_init(&raw_full, 1);
         mbar_init(&raw_empty, 256);
         for (uint32_t i = 0; i < kStagesA; ++i) mbar_init(full_a + i, 256), mbar_init(empty_a + i, 1);
-        for (uint32_t i = 0; i < kStagesB; ++i) mbar_init(full_b + i, 128), mbar_init(empty_b + i, 1);
+        for (uint32_t i = 0; i < kStagesB; ++i) mbar_init(full_b + i, kThreadsX), mbar_init(empty_b + i, 1);
         mbar_init(&done, 1);
         mbar_fence_init();
         failed = 0;
@@ -165,58 +165,76 @@ __global__ void __launch_bounds__(kManyThreads, MT == 1 ? 2 : 1) enec_micro_many
         // x: eight lanes a row of 64 columns
         const uint32_t me = threadIdx.x - kFirstX * 32, c = me & 7;
         const uint32_t first_col = min(k0 * kMicroCols, job.s.cols);
-        uint32_t waiting = 0;   // steps asked for and not announced
-        uint32_t announced = 0;
-        auto announce = [&]() {
-            fence_async_shared();
-            mbar_arrive(full_b + announced % kStagesB);
-            ++announced;
-            --waiting;
-        };
+        const uint8_t* from = job.x + (uint64_t(token0) * job.ld_x + first_col) * 2;
         bool ok = true;
-        for (uint32_t j = 0; j < steps; ++j) {
-            const uint32_t sb = j % kStagesB;
-            if (j >= kStagesB && !suspended_wait(empty_b + sb, (j / kStagesB - 1) & 1, &failed)) {
-                ok = false;
-                break;
-            }
-            const uint32_t dst = smem_u32(b_ring) + sb * n * 128;
-            const uint32_t col = j * 64 + c * 8;                                     // of this CTA's columns
-            const uint32_t valid = col < columns ? min(columns - col, 8u) : 0;
-            if (job.aligned) {
-                const uint8_t* from = job.x + (uint64_t(token0) * job.ld_x + first_col + (valid ? col : 0)) * 2;
+        if (job.aligned) {
+            for (uint32_t j = 0; j < steps; ++j) {
+                const uint32_t sb = j % kStagesB;
+                if (j >= kStagesB && !suspended_wait(empty_b + sb, (j / kStagesB - 1) & 1, &failed)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t dst = smem_u32(b_ring) + sb * n * 128;
+                const uint32_t col = j * 64 + c * 8;                                     // of this CTA's columns
+                const uint32_t valid = col < columns ? min(columns - col, 8u) : 0;
+                const uint8_t* here = from + (valid ? col : 0) * 2;
 #pragma unroll 4
-                for (uint32_t r = me >> 3; r < n; r += 16) {
+                for (uint32_t r = me >> 3; r < n; r += kThreadsX / 8) {
                     const bool real = token0 + r < job.tokens;
-                    cp_async16_some(dst + r * 128 + ((c ^ (r & 7)) << 4), from + (real ? uint64_t(r) * job.ld_x * 2 : 0), real ? valid * 2 : 0);
+                    cp_async16_some(dst + r * 128 + ((c ^ (r & 7)) << 4), here + (real ? uint64_t(r) * job.ld_x * 2 : 0), real ? valid * 2 : 0);
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
-                ++waiting;
-                if (waiting == 2) {   // the step before this one has arrived while this one is on its way
+                if (j > 0) {   // the step before this one has arrived while this one is on its way
                     asm volatile("cp.async.wait_group 1;" ::: "memory");
-                    announce();
+                    fence_async_shared();
+                    mbar_arrive(full_b + (j - 1) % kStagesB);
                 }
-            } else {
-                const uint8_t* from = job.x + (uint64_t(token0) * job.ld_x + first_col + col) * 2;
-                for (uint32_t r0 = me >> 3; r0 < n; r0 += 64) {
+            }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            if (ok && steps > 0) {
+                fence_async_shared();
+                mbar_arrive(full_b + (steps - 1) % kStagesB);
+            }
+        } else {
+            // rows that lie anywhere: through registers, 128 rows of a step at a time, the next ones' loads on the way meanwhile
+            const uint32_t batches = (n + 127) / 128;
+            uint32_t next[4][4];
+            auto load = [&](uint32_t j, uint32_t batch) {
+                const uint32_t col = j * 64 + c * 8;
+                const int valid = col < columns ? int(min(columns - col, 8u)) : 0;
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const uint32_t r = batch * 128 + i * 32 + (me >> 3);
+                    load_eight<DT>(from + (uint64_t(r) * job.ld_x + col) * 2, r < n && token0 + r < job.tokens ? valid : 0, next[i]);
+                }
+            };
+            if (steps > 0) load(0, 0);
+            for (uint32_t j = 0; j < steps && ok; ++j) {
+                const uint32_t sb = j % kStagesB, dst = smem_u32(b_ring) + sb * n * 128;
+                for (uint32_t batch = 0; batch < batches; ++batch) {
                     uint32_t v[4][4];
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i) {
-                        const uint32_t r = r0 + 16 * i;
-                        load_eight<DT>(from + uint64_t(r) * job.ld_x * 2, r < n && token0 + r < job.tokens ? int(valid) : 0, v[i]);
+#pragma unroll
+                        for (uint32_t e = 0; e < 4; ++e) v[i][e] = next[i][e];
+                    }
+                    if (batch + 1 < batches) load(j, batch + 1);
+                    else if (j + 1 < steps) load(j + 1, 0);
+                    if (batch == 0 && j >= kStagesB && !suspended_wait(empty_b + sb, (j / kStagesB - 1) & 1, &failed)) {
+                        ok = false;
+                        break;
                     }
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i) {
-                        const uint32_t r = r0 + 16 * i;
+                        const uint32_t r = batch * 128 + i * 32 + (me >> 3);
                         if (r < n) sts128(dst + r * 128 + ((c ^ (r & 7)) << 4), make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]));
                     }
                 }
-                ++waiting;
-                announce();
+                if (!ok) break;
+                fence_async_shared();
+                mbar_arrive(full_b + sb);
             }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        while (waiting) announce();
         if (!ok) failed = 1;
     } else {
         // the weights: thread (row, half) brings back 32 of the 64 columns of a step, of one row in each 128
@@ -337,8 +355,8 @@ __global__ void __launch_bounds__(kManyThreads, MT == 1 ? 2 : 1) enec_micro_many
             const uint32_t with = (job.s.col_tiles + job.share - 1) / job.share;
             const uint32_t row_in = threadIdx.x & 127;
             const uint32_t row = row_tile * kMicroRows + row_in;
-            if (threadIdx.x < 384 && good && !failed && row < job.s.rows) {
-                for (uint32_t t = (threadIdx.x >> 7) * job.cluster + rank; t < n && token0 + t < job.tokens; t += 3 * job.cluster) {
+            if (threadIdx.x < 512 && good && !failed && row < job.s.rows) {
+                for (uint32_t t = (threadIdx.x >> 7) * job.cluster + rank; t < n && token0 + t < job.tokens; t += 4 * job.cluster) {
                     float v = 0.f;
                     for (uint32_t k = 0; k < with; ++k)
                         v += cluster.map_shared_rank(reinterpret_cast<float*>(smem), k)[t * kMicroRows + row_in];

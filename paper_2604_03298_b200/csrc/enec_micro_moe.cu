@@ -44,8 +44,7 @@ struct MoeJob {
     uint32_t most_slices;            // parts of the columns, at most
     uint32_t ld_h;
     uint32_t* slices;                // the parts that launch 1 has chosen
-    uint32_t* pair_expert;
-    float* pair_weight;
+    uint8_t* tables;                 // launch 1's routing tables
     uint32_t* tickets;               // one per row tile of down
     float* in_sums;                  // [part][gate, up][pair][ld_h]
     float* out_sums;                 // [part][pair][hidden]
@@ -156,10 +155,10 @@ __device__ __forceinline__ void mma_native(float* c, const uint32_t* a0, const u
     }
 }
 
-// The order of logits as numbers without sign; NaN comes last.
+// The order of logits as numbers without sign, from 1 on; NaN comes last. (-infinity is 0x007FFFFF.) 0 is free for what cannot be chosen.
 __device__ __forceinline__ uint32_t logit_key(float v) {
-    const uint32_t b = __float_as_uint(v);
-    if (v != v) return 0;
+    const uint32_t b = __float_as_uint(v == 0.f ? 0.f : v);   // the two zeros are equal
+    if (v != v) return 1;
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
@@ -242,29 +241,34 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
     cluster.sync();
     for (uint32_t token = warp; token < job.tokens; token += kMoeWarps) {
         const float* l = logits + token * job.experts;
-        uint32_t taken = 0;   // bit i: expert lane + 32 i
-        float highest = 0.f, sum = 0.f, mine = 0.f;
+        constexpr uint32_t kMost = kMoeMostExperts / 32;
+        uint32_t keys[kMost];   // of experts lane, lane + 32, ..; 0 for those that do not exist or have been chosen
+#pragma unroll
+        for (uint32_t i = 0; i < kMost; ++i) keys[i] = lane + 32 * i < job.experts ? logit_key(l[lane + 32 * i]) : 0u;
         uint32_t my_expert = 0;
+        float my_logit = 0.f;
         for (uint32_t j = 0; j < job.top; ++j) {
-            uint32_t key = 0, at = 0xFFFFFFFFu;
-            for (uint32_t i = 0; lane + 32 * i < job.experts; ++i) {
-                const uint32_t k = logit_key(l[lane + 32 * i]);
-                if (!(taken >> i & 1) && (at == 0xFFFFFFFFu || k > key)) key = k, at = lane + 32 * i;
+            uint32_t key = 0, at = 0;
+#pragma unroll
+            for (uint32_t i = 0; i < kMost; ++i)
+                if (32 * i < job.experts && keys[i] > key) key = keys[i], at = i;
+            const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, key);
+            const uint32_t chosen = __reduce_min_sync(0xFFFFFFFFu, key == best ? lane + 32 * at : 0xFFFFFFFFu);
+            if ((chosen & 31) == lane) {
+#pragma unroll
+                for (uint32_t i = 0; i < kMost; ++i)
+                    if (i == chosen >> 5) keys[i] = 0;
             }
-            const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, at == 0xFFFFFFFFu ? 0u : key);
-            const uint32_t chosen = __reduce_min_sync(0xFFFFFFFFu, key == best ? at : 0xFFFFFFFFu);
-            if ((chosen & 31) == lane) taken |= 1u << (chosen >> 5);
-            const float v = l[chosen];
-            if (j == 0) highest = v;
-            const float p = expf(v - highest);
-            if (job.renormalize) sum += p;
-            if (lane == j) mine = p, my_expert = chosen;
+            if (lane == j) my_expert = chosen;
         }
-        if (!job.renormalize) {
+        if (lane < job.top) my_logit = l[my_expert];
+        const float highest = __shfl_sync(0xFFFFFFFFu, my_logit, 0);
+        const float mine = lane < job.top ? expf(my_logit - highest) : 0.f;
+        float sum = job.renormalize ? mine : 0.f;
+        if (!job.renormalize)
             for (uint32_t e = lane; e < job.experts; e += 32) sum += expf(l[e] - highest);
 #pragma unroll
-            for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-        }
+        for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
         if (lane < job.top) {
             r.weight[token * job.top + lane] = mine / sum;
             r.expert[token * job.top + lane] = uint16_t(my_expert);
@@ -275,11 +279,11 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
 
 // How many parts a matrix's columns are cut into: what gives the CTA with most tasks the least to do, a task counted as its records and
 // two more for taking its sums.
-__device__ __forceinline__ uint32_t choose_slices(uint64_t tasks, uint32_t records, uint32_t most) {
+__device__ __forceinline__ uint32_t choose_slices(uint32_t tasks, uint32_t records, uint32_t most) {
     uint32_t best = 1;
     uint64_t least = ~uint64_t(0);
     for (uint32_t n = 1; n <= most && n <= records; n *= 2) {
-        const uint64_t cost = (tasks * n + gridDim.x - 1) / gridDim.x * ((records + n - 1) / n + 2);
+        const uint64_t cost = uint64_t((tasks * n + gridDim.x - 1) / gridDim.x) * ((records + n - 1) / n + 2);
         if (cost < least) least = cost, best = n;
     }
     return best;
@@ -291,9 +295,10 @@ struct Tasks {
     uint32_t begin, end;
     __device__ __forceinline__ Tasks(uint32_t groups, uint32_t matrices_, const MicroShape& s, uint32_t slices_)
         : matrices(matrices_), tiles(s.row_tiles), slices(slices_), records(s.col_tiles), share((s.col_tiles + slices_ - 1) / slices_) {
-        const uint64_t all = uint64_t(groups) * matrices * tiles * slices;
-        begin = uint32_t(all * blockIdx.x / gridDim.x);
-        end = uint32_t(all * (blockIdx.x + 1) / gridDim.x);
+        // below 2^32: 1024 groups, two matrices, 2^17 row tiles, eight parts where groups are at most eight
+        const uint32_t all = groups * matrices * tiles * slices, each = all / gridDim.x, more = all % gridDim.x;
+        begin = blockIdx.x * each + min(blockIdx.x, more);
+        end = begin + each + (blockIdx.x < more ? 1 : 0);
     }
 };
 // A walk over a CTA's tasks: divisions once, then counting.
@@ -342,18 +347,19 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_in_kernel(const __g
     piece_setup(sh, job.stages);
     pdl_wait();
     pdl_launch_dependents();
+    const bool good = micro_header_ok(job.gate, job.s_in) && micro_header_ok(job.up, job.s_in);
     route<DT>(job, r, reinterpret_cast<float*>(smem + tables));
     build_lists(r, job.group);
     fence_async_shared();   // the ring's bulk copies go where the router's sums were
     __syncthreads();
     const uint32_t groups = r.group_first[job.experts];
-    const uint32_t slices = choose_slices(uint64_t(groups) * 2 * job.s_in.row_tiles, job.s_in.col_tiles, job.most_slices);
+    const uint32_t slices = choose_slices(groups * 2 * job.s_in.row_tiles, job.s_in.col_tiles, job.most_slices);
     if (blockIdx.x == 0) {
-        for (uint32_t p = threadIdx.x; p < pairs; p += kPieceThreads) job.pair_expert[p] = r.expert[p], job.pair_weight[p] = r.weight[p];
+        for (uint32_t i = threadIdx.x; i < tables / 16; i += kPieceThreads)
+            reinterpret_cast<uint4*>(job.tables)[i] = reinterpret_cast<const uint4*>(smem)[i];
         for (uint32_t i = threadIdx.x; i < job.s_out.row_tiles; i += kPieceThreads) job.tickets[i] = 0;
         if (threadIdx.x == 0) *job.slices = slices;
     }
-    const bool good = micro_header_ok(job.gate, job.s_in) && micro_header_ok(job.up, job.s_in);
     const Tasks tasks(groups, 2, job.s_in, slices);
     const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
     Walk walk(tasks, r, job.group, job.gate, job.up), here = walk;
@@ -393,13 +399,13 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_out_kernel(const __
     piece_setup(sh, job.stages);
     pdl_wait();
     pdl_launch_dependents();
-    for (uint32_t p = threadIdx.x; p < pairs; p += kPieceThreads) r.expert[p] = uint16_t(job.pair_expert[p]), r.weight[p] = job.pair_weight[p];
+    // the tables of launch 1: the groups are the same
+    for (uint32_t i = threadIdx.x; i < tables / 16; i += kPieceThreads) reinterpret_cast<uint4*>(smem)[i] = __ldcg(reinterpret_cast<const uint4*>(job.tables) + i);
     const uint32_t in_slices = *job.slices;
     const bool good = micro_header_ok(job.gate, job.s_in) && micro_header_ok(job.up, job.s_in) && micro_header_ok(job.down, job.s_out);
     __syncthreads();
-    build_lists(r, job.group);
     const uint32_t groups = r.group_first[job.experts];
-    const uint32_t slices = choose_slices(uint64_t(groups) * job.s_out.row_tiles, job.s_out.col_tiles, job.most_slices);
+    const uint32_t slices = choose_slices(groups * job.s_out.row_tiles, job.s_out.col_tiles, job.most_slices);
     const Tasks tasks(groups, 1, job.s_out, slices);
     const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
     Walk walk(tasks, r, job.group, job.down, nullptr), here = walk;
@@ -446,10 +452,18 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_out_kernel(const __
             if (!last || !good || !ok) return;
             __threadfence();
             if (row >= job.hidden) return;
+            const uint32_t terms = job.top * slices;   // of a token: choice by choice, in each part by part; eight loads are on the way together
             for (uint32_t token = worker >> 2; token < job.tokens; token += kPieceWorkers / 4) {
                 float v = 0.f;
-                for (uint32_t j = 0; j < job.top; ++j) {
-                    for (uint32_t s = 0; s < slices; ++s) v += __ldcg(job.out_sums + (uint64_t(s) * pairs + token * job.top + j) * job.hidden + row);
+                for (uint32_t k0 = 0; k0 < terms; k0 += 8) {
+                    float term[8];
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k) {
+                        const uint32_t j = (k0 + k) / slices, s = (k0 + k) % slices;
+                        term[k] = k0 + k < terms ? __ldcg(job.out_sums + (uint64_t(s) * pairs + token * job.top + j) * job.hidden + row) : 0.f;
+                    }
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k) v += term[k];
                 }
                 reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
             }
@@ -514,6 +528,11 @@ enec_status launch_moe(MoeJob job, const MicroDevice& dev, cudaStream_t stream) 
     if (!choose_group(tables, job.s_in.col_tiles, most, router_bytes(job.tokens, job.experts), job.group, job.stages, bytes) ||
         !choose_group(tables, job.s_out.col_tiles, most, 0, second.group, second.stages, bytes2))
         return ENEC_ERR_TOO_LARGE;
+    // one size of group for both launches: the larger rows' decides
+    const uint32_t group = job.group < second.group ? job.group : second.group;
+    if (!choose_group(tables, job.s_in.col_tiles, group, router_bytes(job.tokens, job.experts), job.group, job.stages, bytes) ||
+        !choose_group(tables, job.s_out.col_tiles, group, 0, second.group, second.stages, bytes2) || job.group != second.group)
+        return ENEC_ERR_TOO_LARGE;
     if (!allow_shared(allowed_in, dev, enec_moe_in_kernel<DT>, kFewMostShared) ||
         !allow_shared(allowed_out, dev, enec_moe_out_kernel<DT>, kFewMostShared) ||
         !resident_clusters(enec_moe_in_kernel<DT>, dev, bytes, clusters))
@@ -540,7 +559,7 @@ enec_status launch_moe(MoeJob job, const MicroDevice& dev, cudaStream_t stream) 
 }
 
 struct MoeLayout {
-    uint64_t weight, tickets, in_sums, out_sums, total;
+    uint64_t tickets, in_sums, out_sums, total;
     uint32_t ld_h, most_slices;
 };
 bool moe_layout(uint64_t tokens, uint64_t hidden, uint64_t inter, uint64_t experts, uint64_t top, MoeLayout& l) {
@@ -551,8 +570,7 @@ bool moe_layout(uint64_t tokens, uint64_t hidden, uint64_t inter, uint64_t exper
     // parts of the columns only while pairs are few: with 64 pairs and more there are tasks enough
     l.most_slices = pairs >= 64 ? 1 : pairs > 8 ? uint32_t(64 / pairs) : 8;
     l.ld_h = uint32_t((inter + 3) & ~uint64_t(3));
-    l.weight = 16 + align16(pairs * 4);
-    l.tickets = l.weight + align16(pairs * 4);
+    l.tickets = 16 + routing_bytes(uint32_t(pairs), uint32_t(experts));
     l.in_sums = l.tickets + align16((hidden + kMicroRows) / kMicroRows * 4);
     l.out_sums = l.in_sums + l.most_slices * 2 * pairs * l.ld_h * 4;
     l.total = l.out_sums + align16(l.most_slices * pairs * hidden * 4);
@@ -608,8 +626,7 @@ extern "C" enec_status enec_moe_microscaled(const void* d_x, enec_dtype dt, size
     job.most_slices = l.most_slices;
     job.ld_h = l.ld_h;
     job.slices = reinterpret_cast<uint32_t*>(ws);
-    job.pair_expert = reinterpret_cast<uint32_t*>(ws + 16);
-    job.pair_weight = reinterpret_cast<float*>(ws + l.weight);
+    job.tables = ws + 16;
     job.tickets = reinterpret_cast<uint32_t*>(ws + l.tickets);
     job.in_sums = reinterpret_cast<float*>(ws + l.in_sums);
     job.out_sums = reinterpret_cast<float*>(ws + l.out_sums);
