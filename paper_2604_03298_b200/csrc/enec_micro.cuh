@@ -83,14 +83,18 @@ inline bool allow_shared(std::atomic<uint64_t>& done, const MicroDevice& dev, Ke
 
 #ifdef __CUDACC__
 
-// Whether the header says what the call says. The host has checked the stream's size against the shape, so every read of the
-// records is in bounds whatever the header holds: kernels load first and ask this before they store.
-__device__ __forceinline__ bool micro_header_ok(const uint8_t* stream, const MicroShape& s) {
-    const uint4 a = *reinterpret_cast<const uint4*>(stream);
-    const uint4 b = *reinterpret_cast<const uint4*>(stream + 16);
-    return a.x == kMicroMagic && a.y == kMicroVersion && a.z == s.batch && a.w == s.rows && b.x == s.cols && b.y == 0 &&
-           b.z == uint32_t(s.total) && b.w == uint32_t(s.total >> 32);
-}
+// The header's first 32 bytes, loaded early and looked at late. The host has checked the stream's size against the shape, so every read of
+// the records is in bounds whatever the header holds: kernels work first and ask whether it says what the call says before they store.
+struct MicroProbe {
+    uint4 a, b;
+    __device__ __forceinline__ explicit MicroProbe(const uint8_t* stream)
+        : a(*reinterpret_cast<const uint4*>(stream)), b(*reinterpret_cast<const uint4*>(stream + 16)) {}
+    __device__ __forceinline__ bool fits(const MicroShape& s) const {
+        return a.x == kMicroMagic && a.y == kMicroVersion && a.z == s.batch && a.w == s.rows && b.x == s.cols && b.y == 0 &&
+               b.z == uint32_t(s.total) && b.w == uint32_t(s.total >> 32);
+    }
+};
+__device__ __forceinline__ bool micro_header_ok(const uint8_t* stream, const MicroShape& s) { return MicroProbe(stream).fits(s); }
 
 // 2^(byte - 127); byte 0 is a subnormal number of fp32, byte 255 stands for not-a-number.
 __device__ __forceinline__ float micro_scale(uint32_t byte) {

@@ -1,8 +1,8 @@
 // y = x W^T for few tokens, W a microscaled stream: one launch that reads every weight once (see enec_micro_pieces.cuh).
 //
 // A CTA takes row tiles of W, one after another. Where there are fewer of them than SMs, or where the digits of whole rows of x would not
-// fit into shared memory, a cluster of CTAs shares the columns: each leaves its sums in its shared memory and adds up a part of the
-// tokens, in the order of the CTAs. No sum depends on which CTA was faster.
+// fit into shared memory, a cluster of CTAs shares the columns: each sends its sums to the CTA that adds up the token's, in the
+// order of the CTAs. No sum depends on which CTA was faster.
 #include "enec_micro_pieces.cuh"
 
 #include <cooperative_groups.h>
@@ -45,50 +45,62 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_micro_few_kernel(const 
     const uint32_t n_tasks = (job.s.row_tiles - first_tile + step - 1) / step;
     const uint32_t first = min(rank * job.share, job.s.col_tiles), count = min(job.share, job.s.col_tiles - first);
     const uint64_t tile_bytes = uint64_t(job.s.col_tiles) * kMicroRecordBytes;
-    const uint32_t columns = piece_columns(job.tokens), record_bytes = piece_record_bytes(job.tokens);
-    float* sums = reinterpret_cast<float*>(smem + job.stages * kMicroRecordBytes + job.share * record_bytes);   // two sets of [token][row]
+    // two sets of [CTA][token][row]
+    float* sums = reinterpret_cast<float*>(smem + job.stages * kMicroRecordBytes + job.share * piece_record_bytes(job.tokens));
+    // other CTAs' shared memory may be written once they have begun
+    if (job.cluster > 1) cooperative_groups::this_cluster().barrier_arrive();
     piece_setup(sh, job.stages);
     pdl_wait();
     pdl_launch_dependents();
-    const bool good = micro_header_ok(job.w, job.s);
+    const MicroProbe header(job.w);
+    const uint32_t owned = (job.tokens + job.cluster - 1) / job.cluster;   // tokens that a CTA of the cluster adds up, at most
     const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
+    if (job.cluster > 1) cooperative_groups::this_cluster().barrier_wait();
     piece_products(
         sh, smem, job.stages, n_tasks, job.s.cols,
-        FewTasks{PieceTask{job.w + kMicroHeaderBytes + first_tile * tile_bytes, first, count, 0, 0}, step * tile_bytes},
-        [&](uint32_t, uint32_t at) {
-            stage_rows<DT>(worker, lane, count, job.tokens, at, [&](uint32_t c) { return job.x + uint64_t(c) * job.ld_x * 2; }, first, job.s.cols);
+        FewTasks{PieceTask{job.w + kMicroHeaderBytes + first_tile * tile_bytes, first, count, 0, job.tokens}, step * tile_bytes},
+        [&](uint32_t token, uint32_t col, float* x) {
+            uint32_t w[4];
+            load_eight<DT>(job.x + (uint64_t(token) * job.ld_x + col) * 2, col < job.s.cols ? int(min(job.s.cols - col, 8u)) : 0, w);
+            as_floats<DT>(w, x);
         },
-        [&](uint32_t) { return columns; },
         [&](uint32_t i, uint32_t tmem, bool ok) {
             const uint32_t row = (first_tile + i * step) * kMicroRows + row_in;
             for (uint32_t token = worker >> 2; token < job.tokens; token += kPieceWorkers / 4) {
                 const float v = count ? take_sum(tmem, token) : 0.f;
-                if (job.cluster > 1) sums[((i & 1) * job.tokens + token) * kMicroRows + row_in] = v;
-                else if (good && ok && row < job.s.rows) reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
+                if (job.cluster > 1) {   // to the CTA that adds up this token
+                    float* to = cooperative_groups::this_cluster().map_shared_rank(sums, token % job.cluster);
+                    to[(((i & 1) * job.cluster + rank) * owned + token / job.cluster) * kMicroRows + row_in] = v;
+                } else if (header.fits(job.s) && ok && row < job.s.rows) {
+                    reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
+                }
             }
         },
         [](uint32_t, bool) {}, job.cluster > 1,
         [&](uint32_t i) {
-            auto cluster = cooperative_groups::this_cluster();
-            cluster.sync();   // a set of sums is written again behind the next one of these, and has been read by then
+            // a set of sums is written again behind the next one of these, and has been read by then; nothing comes from other CTAs behind
+            // the last one
+            cooperative_groups::this_cluster().sync();
             const uint32_t r = threadIdx.x & 127, row = (first_tile + i * step) * kMicroRows + r;
-            if (threadIdx.x >= 512 || row >= job.s.rows || !good || sh.failed) return;
-            for (uint32_t token = (threadIdx.x >> 7) * job.cluster + rank; token < job.tokens; token += 4 * job.cluster) {
+            if (threadIdx.x >= 512 || row >= job.s.rows || !header.fits(job.s) || sh.failed) return;
+            for (uint32_t t = threadIdx.x >> 7; t * job.cluster + rank < job.tokens; t += 4) {
+                const float* from = sums + ((i & 1) * job.cluster * owned + t) * kMicroRows + r;
                 float v = 0.f;
-                for (uint32_t k = 0; k < job.cluster; ++k) v += cluster.map_shared_rank(sums, k)[((i & 1) * job.tokens + token) * kMicroRows + r];
-                reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k)
+                    if (k < job.cluster) v += from[k * owned * kMicroRows];
+                reinterpret_cast<T*>(job.y)[uint64_t(t * job.cluster + rank) * job.ld_y + row] = MicroType<DT>::one(v);
             }
         });
     if (threadIdx.x == 0) {
         if (sh.failed) report(job.status, ENEC_ERR_TIMEOUT);
-        else if (!good && blockIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
+        else if (!header.fits(job.s) && blockIdx.x == 0) report(job.status, ENEC_ERR_BAD_STREAM);
     }
-    if (job.cluster > 1) cooperative_groups::this_cluster().sync();   // no CTA ends while its sums are read
 }
 
 // Shared memory of a CTA that takes `share` records with four stages, or 0 where it does not fit.
 uint32_t few_bytes(uint32_t share, uint32_t tokens, uint32_t cluster, uint32_t& stages) {
-    const uint64_t others = 1024 + uint64_t(share) * piece_record_bytes(tokens) + (cluster > 1 ? tokens * kMicroRows * 8 : 0);
+    const uint64_t others = 1024 + uint64_t(share) * piece_record_bytes(tokens) + (cluster > 1 ? (tokens + cluster - 1) / cluster * cluster * kMicroRows * 8 : 0);
     if (others + 4 * kMicroRecordBytes > kFewMostShared) return 0;
     const uint64_t fit = (kFewMostShared - others) / kMicroRecordBytes;
     stages = fit < kPieceMostStages ? uint32_t(fit) : kPieceMostStages;

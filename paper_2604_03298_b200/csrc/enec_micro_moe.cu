@@ -171,6 +171,30 @@ __host__ __device__ inline uint32_t router_bytes(uint32_t tokens, uint32_t exper
     return (1 + router_splits(tokens, experts)) * tokens * experts * 4;
 }
 
+// A warp: the `top` largest of `experts` logits, ties to the lower number; lane j gets the j-th. N: experts a lane looks after.
+template <uint32_t N>
+__device__ __forceinline__ uint32_t choose_experts(const float* l, uint32_t experts, uint32_t top, uint32_t lane) {
+    uint32_t keys[N];   // of experts lane, lane + 32, ..; 0 for those that do not exist or have been chosen
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) keys[i] = lane + 32 * i < experts ? logit_key(l[lane + 32 * i]) : 0u;
+    uint32_t mine = 0;
+    for (uint32_t j = 0; j < top; ++j) {
+        uint32_t key = 0, at = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) {
+            at = keys[i] > key ? i : at;
+            key = max(keys[i], key);
+        }
+        const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, key);
+        const uint32_t chosen = __reduce_min_sync(0xFFFFFFFFu, key == best ? lane + 32 * at : 0xFFFFFFFFu);
+        const uint32_t gone = (chosen & 31) == lane ? chosen >> 5 : N;
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) keys[i] = i == gone ? 0u : keys[i];
+        mine = lane == j ? chosen : mine;
+    }
+    return mine;
+}
+
 // The router: logits of all tokens to every CTA of the cluster, then every warp chooses for its tokens.
 template <int DT>
 __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float* scratch) {
@@ -226,41 +250,30 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
             if (ee < job.experts && tt < job.tokens) part[split * total + tt * job.experts + ee] = c[i];
         }
     }
+    if (splits > 1) {
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < total; i += blockDim.x) {
+            float v = part[i];
+            for (uint32_t s = 1; s < splits; ++s) v += part[s * total + i];
+            part[i] = v;
+        }
+    }
     cluster.sync();
     const uint32_t per = (total + kMoeCluster - 1) / kMoeCluster;
     for (uint32_t i = rank * per + threadIdx.x; i < min(total, (rank + 1) * per); i += blockDim.x) {
         float v = 0.f;
 #pragma unroll
-        for (uint32_t k = 0; k < kMoeCluster; ++k) {
-            const float* theirs = cluster.map_shared_rank(part, k);
-            for (uint32_t s = 0; s < splits; ++s) v += theirs[s * total + i];
-        }
+        for (uint32_t k = 0; k < kMoeCluster; ++k) v += cluster.map_shared_rank(part, k)[i];
 #pragma unroll
         for (uint32_t k = 0; k < kMoeCluster; ++k) cluster.map_shared_rank(logits, k)[i] = v;
     }
     cluster.sync();
     for (uint32_t token = warp; token < job.tokens; token += kMoeWarps) {
         const float* l = logits + token * job.experts;
-        constexpr uint32_t kMost = kMoeMostExperts / 32;
-        uint32_t keys[kMost];   // of experts lane, lane + 32, ..; 0 for those that do not exist or have been chosen
-#pragma unroll
-        for (uint32_t i = 0; i < kMost; ++i) keys[i] = lane + 32 * i < job.experts ? logit_key(l[lane + 32 * i]) : 0u;
-        uint32_t my_expert = 0;
+        const uint32_t my_expert = job.experts <= 64    ? choose_experts<2>(l, job.experts, job.top, lane)
+                                   : job.experts <= 128 ? choose_experts<4>(l, job.experts, job.top, lane)
+                                                        : choose_experts<kMoeMostExperts / 32>(l, job.experts, job.top, lane);
         float my_logit = 0.f;
-        for (uint32_t j = 0; j < job.top; ++j) {
-            uint32_t key = 0, at = 0;
-#pragma unroll
-            for (uint32_t i = 0; i < kMost; ++i)
-                if (32 * i < job.experts && keys[i] > key) key = keys[i], at = i;
-            const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, key);
-            const uint32_t chosen = __reduce_min_sync(0xFFFFFFFFu, key == best ? lane + 32 * at : 0xFFFFFFFFu);
-            if ((chosen & 31) == lane) {
-#pragma unroll
-                for (uint32_t i = 0; i < kMost; ++i)
-                    if (i == chosen >> 5) keys[i] = 0;
-            }
-            if (lane == j) my_expert = chosen;
-        }
         if (lane < job.top) my_logit = l[my_expert];
         const float highest = __shfl_sync(0xFFFFFFFFu, my_logit, 0);
         const float mine = lane < job.top ? expf(my_logit - highest) : 0.f;
@@ -280,16 +293,15 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
 // How many parts a matrix's columns are cut into: what gives the CTA with most tasks the least to do, a task counted as its records and
 // two more for taking its sums.
 __device__ __forceinline__ uint32_t choose_slices(uint32_t tasks, uint32_t records, uint32_t most) {
-    uint32_t best = 1;
-    uint64_t least = ~uint64_t(0);
-    for (uint32_t n = 1; n <= most && n <= records; n *= 2) {
-        const uint64_t cost = uint64_t((tasks * n + gridDim.x - 1) / gridDim.x) * ((records + n - 1) / n + 2);
-        if (cost < least) least = cost, best = n;
-    }
-    return best;
+    if (most == 1) return 1;
+    const uint32_t lane = threadIdx.x & 31, n = 1u << (lane & 3);   // by whole warps: lanes 0 to 3 look at 1, 2, 4 and 8 parts
+    uint32_t cost = 0xFFFFFFFFu;
+    if (n <= most && n <= records) cost = (tasks * n + gridDim.x - 1) / gridDim.x * ((records + n - 1) / n + 2);
+    const uint32_t least = __reduce_min_sync(0xFFFFFFFFu, cost);
+    return 1u << __reduce_min_sync(0xFFFFFFFFu, cost == least ? lane & 3 : 3u);
 }
 
-// The tasks of a launch, in the order group, matrix, row tile, part of the columns; and a CTA's share of them.
+// The tasks of a launch, in the order group, part of the columns, matrix, row tile; and a CTA's share of them.
 struct Tasks {
     uint32_t matrices, tiles, slices, records, share;
     uint32_t begin, end;
@@ -312,26 +324,26 @@ struct Walk {
     Group now;
     __device__ __forceinline__ Walk(const Tasks& tasks_, const Routing& r_, uint32_t group_size_, const uint8_t* m0_, const uint8_t* m1_)
         : tasks(tasks_), r(r_), group_size(group_size_), m0(m0_), m1(m1_) {
-        slice = tasks.begin % tasks.slices;
-        const uint32_t rest = tasks.begin / tasks.slices;
-        tile = rest % tasks.tiles;
-        matrix = rest / tasks.tiles % tasks.matrices;
-        group = rest / tasks.tiles / tasks.matrices;
+        tile = tasks.begin % tasks.tiles;
+        uint32_t rest = tasks.begin / tasks.tiles;
+        matrix = rest % tasks.matrices, rest /= tasks.matrices;
+        slice = rest % tasks.slices;
+        group = rest / tasks.slices;
         if (tasks.begin < tasks.end) now = group_of(r, group, group_size);
     }
     __device__ __forceinline__ PieceTask get() const {
         const uint32_t first = min(slice * tasks.share, tasks.records);
         const uint64_t strip = uint64_t(now.expert) * tasks.tiles + tile;
-        return {(matrix ? m1 : m0) + kMicroHeaderBytes + strip * tasks.records * kMicroRecordBytes, first, min(tasks.share, tasks.records - first), group,
-                first};
+        return {(matrix ? m1 : m0) + kMicroHeaderBytes + strip * tasks.records * kMicroRecordBytes, first, min(tasks.share, tasks.records - first),
+                group * tasks.slices + slice, now.n};
     }
     __device__ __forceinline__ void next() {
-        if (++slice < tasks.slices) return;
-        slice = 0;
         if (++tile < tasks.tiles) return;
         tile = 0;
         if (++matrix < tasks.matrices) return;
         matrix = 0;
+        if (++slice < tasks.slices) return;
+        slice = 0;
         if (++group < r.group_first[r.experts]) now = group_of(r, group, group_size);
     }
 };
@@ -347,7 +359,7 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_in_kernel(const __g
     piece_setup(sh, job.stages);
     pdl_wait();
     pdl_launch_dependents();
-    const bool good = micro_header_ok(job.gate, job.s_in) && micro_header_ok(job.up, job.s_in);
+    const MicroProbe gate_header(job.gate), up_header(job.up);
     route<DT>(job, r, reinterpret_cast<float*>(smem + tables));
     build_lists(r, job.group);
     fence_async_shared();   // the ring's bulk copies go where the router's sums were
@@ -360,16 +372,18 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_in_kernel(const __g
         for (uint32_t i = threadIdx.x; i < job.s_out.row_tiles; i += kPieceThreads) job.tickets[i] = 0;
         if (threadIdx.x == 0) *job.slices = slices;
     }
+    const bool good = gate_header.fits(job.s_in) && up_header.fits(job.s_in);
     const Tasks tasks(groups, 2, job.s_in, slices);
     const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
     Walk walk(tasks, r, job.group, job.gate, job.up), here = walk;
     piece_products(
         sh, smem + tables, job.stages, tasks.end - tasks.begin, job.hidden, walk,
-        [&](uint32_t, uint32_t at) {
-            stage_rows<DT>(worker, lane, tasks.records, here.now.n, at,
-                           [&](uint32_t c) { return job.x + uint64_t(r.list[here.now.first + c] / job.top) * job.ld_x * 2; }, 0, job.hidden);
+        [&](uint32_t c, uint32_t col, float* x) {
+            uint32_t w[4];
+            load_eight<DT>(job.x + (uint64_t(r.list[here.now.first + c] / job.top) * job.ld_x + col) * 2,
+                           col < job.hidden ? int(min(job.hidden - col, 8u)) : 0, w);
+            as_floats<DT>(w, x);
         },
-        [&](uint32_t group) { return piece_columns(group_of(r, group, job.group).n); },
         [&](uint32_t, uint32_t tmem, bool ok) {
             const uint32_t row = here.tile * kMicroRows + row_in;
             const bool any = here.slice * tasks.share < tasks.records;
@@ -402,36 +416,33 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_out_kernel(const __
     // the tables of launch 1: the groups are the same
     for (uint32_t i = threadIdx.x; i < tables / 16; i += kPieceThreads) reinterpret_cast<uint4*>(smem)[i] = __ldcg(reinterpret_cast<const uint4*>(job.tables) + i);
     const uint32_t in_slices = *job.slices;
-    const bool good = micro_header_ok(job.gate, job.s_in) && micro_header_ok(job.up, job.s_in) && micro_header_ok(job.down, job.s_out);
+    const MicroProbe gate_header(job.gate), up_header(job.up), down_header(job.down);
     __syncthreads();
     const uint32_t groups = r.group_first[job.experts];
     const uint32_t slices = choose_slices(groups * job.s_out.row_tiles, job.s_out.col_tiles, job.most_slices);
+    const bool good = gate_header.fits(job.s_in) && up_header.fits(job.s_in) && down_header.fits(job.s_out);
     const Tasks tasks(groups, 1, job.s_out, slices);
     const uint32_t worker = warp - 2, row_in = (warp & 3) * 32 + lane;
     Walk walk(tasks, r, job.group, job.down, nullptr), here = walk;
     piece_products(
         sh, smem + tables, job.stages, tasks.end - tasks.begin, job.inter, walk,
-        [&](uint32_t, uint32_t at) {
-            const uint32_t n = here.now.n, columns = piece_columns(n), record_bytes = piece_record_bytes(n);
-            for (uint32_t task = worker; task < tasks.records * n; task += kPieceWorkers) {
-                const uint32_t k = task / n, c = task % n;
-                const uint32_t col = k * kMicroCols + 8 * lane;
-                const int valid = col < job.inter ? int(min(job.inter - col, 8u)) : 0;
-                float a[8] = {}, u[8] = {};
-                for (uint32_t s = 0; s < in_slices; ++s) {
-                    const float* from = job.in_sums + (uint64_t(s * 2) * pairs + r.list[here.now.first + c]) * job.ld_h + col;
-                    uint32_t wa[8], wu[8];
-                    load_eight<ENEC_FP32>(reinterpret_cast<const uint8_t*>(from), valid, wa);
-                    load_eight<ENEC_FP32>(reinterpret_cast<const uint8_t*>(from + uint64_t(pairs) * job.ld_h), valid, wu);
+        [&](uint32_t c, uint32_t col, float* x) {
+            const int valid = col < job.inter ? int(min(job.inter - col, 8u)) : 0;
+            const float* from = job.in_sums + uint64_t(r.list[here.now.first + c]) * job.ld_h + col;
+            const uint64_t matrix = uint64_t(pairs) * job.ld_h;
+            float u[8] = {};
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) a[e] += __uint_as_float(wa[e]), u[e] += __uint_as_float(wu[e]);
-                }
+            for (int e = 0; e < 8; ++e) x[e] = 0.f;
+            for (uint32_t s = 0; s < in_slices; ++s, from += 2 * matrix) {
+                uint32_t wa[8], wu[8];
+                load_eight<ENEC_FP32>(reinterpret_cast<const uint8_t*>(from), valid, wa);
+                load_eight<ENEC_FP32>(reinterpret_cast<const uint8_t*>(from + matrix), valid, wu);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] = a[e] / (1.f + expf(-a[e])) * u[e];
-                put_digits(a, c, at + k * record_bytes, columns, lane);
+                for (int e = 0; e < 8; ++e) x[e] += __uint_as_float(wa[e]), u[e] += __uint_as_float(wu[e]);
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = x[e] / (1.f + expf(-x[e])) * u[e];
         },
-        [&](uint32_t group) { return piece_columns(group_of(r, group, job.group).n); },
         [&](uint32_t, uint32_t tmem, bool) {
             const uint32_t row = here.tile * kMicroRows + row_in;
             const bool any = here.slice * tasks.share < tasks.records;
@@ -452,18 +463,22 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_out_kernel(const __
             if (!last || !good || !ok) return;
             __threadfence();
             if (row >= job.hidden) return;
-            const uint32_t terms = job.top * slices;   // of a token: choice by choice, in each part by part; eight loads are on the way together
+            // a token's pairs in the order of its choice, each part by part; loads of eight pairs are on the way together
+#pragma unroll 2
             for (uint32_t token = worker >> 2; token < job.tokens; token += kPieceWorkers / 4) {
+                const float* from = job.out_sums + uint64_t(token) * job.top * job.hidden + row;
                 float v = 0.f;
-                for (uint32_t k0 = 0; k0 < terms; k0 += 8) {
+                for (uint32_t j0 = 0; j0 < job.top; j0 += 8) {
                     float term[8];
 #pragma unroll
-                    for (uint32_t k = 0; k < 8; ++k) {
-                        const uint32_t j = (k0 + k) / slices, s = (k0 + k) % slices;
-                        term[k] = k0 + k < terms ? __ldcg(job.out_sums + (uint64_t(s) * pairs + token * job.top + j) * job.hidden + row) : 0.f;
+                    for (uint32_t j = 0; j < 8; ++j) term[j] = j0 + j < job.top ? __ldcg(from + uint64_t(j0 + j) * job.hidden) : 0.f;
+                    for (uint32_t s = 1; s < slices; ++s) {
+#pragma unroll
+                        for (uint32_t j = 0; j < 8; ++j)
+                            if (j0 + j < job.top) term[j] += __ldcg(from + (uint64_t(s) * pairs + j0 + j) * job.hidden);
                     }
 #pragma unroll
-                    for (uint32_t k = 0; k < 8; ++k) v += term[k];
+                    for (uint32_t j = 0; j < 8; ++j) v += term[j];
                 }
                 reinterpret_cast<T*>(job.y)[uint64_t(token) * job.ld_y + row] = MicroType<DT>::one(v);
             }

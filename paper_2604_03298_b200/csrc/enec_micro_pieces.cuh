@@ -26,6 +26,7 @@ namespace enec {
 constexpr uint32_t kPieces = 8;
 constexpr uint32_t kPieceTokens = 16;        // columns of x that a CTA takes: 128 of the accumulator
 constexpr uint32_t kPieceMostStages = 8;
+constexpr uint32_t kPieceBatches = 16;       // in which a group's digits are announced to the matrix instructions, at most
 constexpr uint32_t kPieceWorkers = 16;       // warps
 constexpr uint32_t kPieceThreads = (2 + kPieceWorkers) * 32;
 constexpr uint32_t kPieceTmem = 512;         // columns: two sets of 128 sums, 16 of scales for each stage
@@ -37,7 +38,7 @@ __host__ __device__ constexpr uint32_t piece_record_bytes(uint32_t tokens) { ret
 #ifdef __CUDACC__
 
 struct PieceShared {
-    uint64_t full[kPieceMostStages], empty[kPieceMostStages], staged, done[2], drained[2];
+    uint64_t full[kPieceMostStages], empty[kPieceMostStages], staged[kPieceBatches], done[2], drained[2];
     uint32_t tmem;
     volatile int failed;
 };
@@ -46,14 +47,14 @@ struct PieceShared {
 struct PieceTask {
     const uint8_t* records;
     uint32_t first, count;
-    uint32_t group;        // tasks of the same group use the same digits
-    uint32_t digits;       // of the staged records the one that belongs to `first`
+    uint32_t group;        // tasks of the same group have the same records and use the same digits
+    uint32_t n;            // columns of x, a group's
 };
 
 __device__ __forceinline__ void piece_setup(PieceShared& sh, uint32_t stages) {
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < stages; ++i) mbar_init(sh.full + i, 1), mbar_init(sh.empty + i, 1);
-        mbar_init(&sh.staged, kPieceWorkers * 32);
+        for (uint32_t i = 0; i < kPieceBatches; ++i) mbar_init(sh.staged + i, kPieceWorkers * 32);
         for (uint32_t i = 0; i < 2; ++i) mbar_init(sh.done + i, 1), mbar_init(sh.drained + i, kPieceWorkers * 32);
         mbar_fence_init();
         sh.failed = 0;
@@ -127,28 +128,41 @@ __device__ __forceinline__ void put_digits(const float* x, uint32_t column, uint
     }
 }
 
-// The workers' part of staging `n` columns over `count` records from `first` on: column c's values (16 bits) are row_of(c)'s, zeros behind
-// `cols`. Two at a time: their loads are on the way together.
-template <int DT, class RowOf>
-__device__ __forceinline__ void stage_rows(uint32_t worker, uint32_t lane, uint32_t count, uint32_t n, uint32_t at, RowOf row_of, uint32_t first,
-                                           uint32_t cols) {
-    const uint32_t columns = piece_columns(n), record_bytes = piece_record_bytes(n), total = count * n;
-    for (uint32_t task = worker; task < total; task += 2 * kPieceWorkers) {
-        uint32_t w[2][4];
+// A group's records x columns are staged in sweeps, two by every worker warp (their loads are on the way together), and announced in
+// batches of sweeps, so that the products of the first records run while the last ones' digits are made.
+struct PieceSweeps {
+    uint32_t total, per_batch, batches, reciprocal;
+    __device__ __forceinline__ PieceSweeps(uint32_t count, uint32_t n) {
+        total = count * n;
+        const uint32_t sweeps = (total + 2 * kPieceWorkers - 1) / (2 * kPieceWorkers);
+        per_batch = (sweeps + kPieceBatches - 1) / kPieceBatches;
+        batches = per_batch ? (sweeps + per_batch - 1) / per_batch : 0;
+        reciprocal = 65536 / n + 1;   // i * reciprocal >> 16 = i / n below 65536 / n, far more than shared memory holds
+    }
+    __device__ __forceinline__ uint32_t batch_of(uint32_t record, uint32_t n) const { return ((record + 1) * n - 1) / (2 * kPieceWorkers) / per_batch; }
+};
+template <class Values>
+__device__ __forceinline__ void stage_digits(PieceShared& sh, uint32_t worker, uint32_t lane, const PieceTask& task, uint32_t at, Values values) {
+    const uint32_t n = task.n, columns = piece_columns(n), record_bytes = piece_record_bytes(n);
+    const PieceSweeps sweeps(task.count, n);
+    for (uint32_t batch = 0; batch < sweeps.batches; ++batch) {
+        for (uint32_t s = 0; s < sweeps.per_batch; ++s) {
+            const uint32_t first = (batch * sweeps.per_batch + s) * 2 * kPieceWorkers + worker;
+            float x[2][8];
+            uint32_t record[2], column[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t here = task + j * kPieceWorkers;
-            const uint32_t col = (first + here / n) * kMicroCols + 8 * lane;
-            load_eight<DT>(here < total ? row_of(here % n) + uint64_t(col) * 2 : nullptr, here < total && col < cols ? int(min(cols - col, 8u)) : 0, w[j]);
-        }
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t i = first + j * kPieceWorkers;
+                record[j] = i * sweeps.reciprocal >> 16;
+                column[j] = i - record[j] * n;
+                if (i < sweeps.total) values(column[j], (task.first + record[j]) * kMicroCols + 8 * lane, x[j]);
+            }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t here = task + j * kPieceWorkers;
-            if (here >= total) break;
-            float x[8];
-            as_floats<DT>(w[j], x);
-            put_digits(x, here % n, at + here / n * record_bytes, columns, lane);
+            for (int j = 0; j < 2; ++j)
+                if (first + j * kPieceWorkers < sweeps.total) put_digits(x[j], column[j], at + record[j] * record_bytes, columns, lane);
         }
+        fence_async_shared();
+        mbar_arrive(sh.staged + batch);
     }
 }
 
@@ -165,14 +179,13 @@ __device__ __forceinline__ float take_sum(uint32_t tmem, uint32_t column) {
     return sum;
 }
 
-// All roles of a CTA over its tasks. tasks: where the first one is, with get() and next(); every role walks a copy. stage(i, at): called by
-// the workers' warps where a group begins, writes the digits of its records to `at` on. columns_of(group): columns of the accumulator it
-// has, a multiple of 16. take(i, tmem, ok): by the workers, takes the sums from their lanes of tensor memory; where not ok, a wait
-// has run out and they are nothing. after(i, ok): by the workers, once the sums' place is free again. meet(i): by all threads behind
-// every task where `lockstep`. smem: the ring, then the digits. cols: of the matrices.
-template <class Tasks, class Stage, class ColumnsOf, class Take, class After, class Meet>
+// All roles of a CTA over its tasks. tasks: where the first one is, with get() and next(); every role walks a copy. values(c, col, x): by
+// the workers, eight values of a group's column c from `col` on. take(i, tmem, ok): by the workers, takes the sums from their lanes of
+// tensor memory; where not ok, a wait has run out and they are nothing. after(i, ok): by the workers, once the sums' place is free
+// again. meet(i): by all threads behind every task where `lockstep`. smem: the ring, then the digits. cols: of the matrices.
+template <class Tasks, class Values, class Take, class After, class Meet>
 __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, uint32_t stages, uint32_t n_tasks, uint32_t cols, Tasks tasks,
-                                               Stage stage, ColumnsOf columns_of, Take take, After after, bool lockstep, Meet meet) {
+                                               Values values, Take take, After after, bool lockstep, Meet meet) {
     const uint32_t warp = threadIdx.x >> 5;
     const uint32_t ring = smem_u32(smem), digits = ring + stages * kMicroRecordBytes;
     const uint32_t tmem = sh.tmem;
@@ -201,21 +214,28 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
     } else if (warp == 1) {
         const uint64_t ring_desc = operand_desc(ring), ring_scales_desc = scale_desc(ring + kMicroElemBytes);
         const uint64_t digits_desc = operand_desc(digits), digit_scales_desc = scale_desc(digits);
-        uint32_t group = 0xFFFFFFFFu, groups = 0, columns = 0, slot = 0, phase = 0;
+        uint32_t group = 0xFFFFFFFFu, slot = 0, phase = 0;
+        uint32_t flipped = 0;   // bit b: announcements of batch b so far, mod 2
         volatile int never = 0;
         for (uint32_t i = 0; i < n_tasks; ++i, tasks.next()) {
             const PieceTask task = tasks.get();
-            if (task.group != group) {
-                group = task.group, columns = columns_of(group);
-                if (!suspended_wait(&sh.staged, groups++ & 1, &sh.failed)) sh.failed = 1;
-            }
+            const uint32_t columns = piece_columns(task.n);
+            const PieceSweeps sweeps(task.count, task.n);
+            const bool begins = task.group != group;
+            group = task.group;
+            uint32_t known = begins ? 0 : sweeps.batches;   // batches that have been waited for
             const uint32_t set = i & 1, sums = tmem + set * (kPieceTokens * kPieces);
             if (i >= 2 && !suspended_wait(sh.drained + set, ((i >> 1) - 1) & 1, &sh.failed)) sh.failed = 1;
             tcgen05_fence_after();
             const uint32_t idesc = scaled_idesc(columns), record16 = columns * 8 + 64;   // a record's digits in units of 16 bytes
-            uint64_t b = digits_desc + task.digits * record16, bs = digit_scales_desc + columns * 8 + task.digits * record16;
+            uint64_t b = digits_desc, bs = digit_scales_desc + columns * 8;
             for (uint32_t k = 0; k < task.count && !sh.failed; ++k) {
-                if (!suspended_wait(sh.full + slot, phase, &sh.failed)) {
+                bool there = suspended_wait(sh.full + slot, phase, &sh.failed);
+                if (known < sweeps.batches) {
+                    const uint32_t batch = sweeps.batch_of(k, task.n);
+                    for (; there && known <= batch; ++known) there = suspended_wait(sh.staged + known, flipped >> known & 1, &sh.failed);
+                }
+                if (!there) {
                     sh.failed = 1;
                     break;
                 }
@@ -237,6 +257,7 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
                 b += record16, bs += record16;
                 if (++slot == stages) slot = 0, phase ^= 1;
             }
+            if (begins) flipped ^= (1u << sweeps.batches) - 1;
             tcgen05_commit(leader, sh.done + set);
             if (lockstep) meet(i);
         }
@@ -248,9 +269,7 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
             const PieceTask task = tasks.get();
             if (task.group != group) {
                 group = task.group;
-                stage(i, digits);
-                fence_async_shared();
-                mbar_arrive(&sh.staged);
+                stage_digits(sh, warp - 2, threadIdx.x & 31, task, digits, values);
             }
             const uint32_t set = i & 1;
             if (!suspended_wait(sh.done + set, (i >> 1) & 1, &sh.failed)) sh.failed = 1;
