@@ -59,27 +59,28 @@ __device__ __forceinline__ uint32_t fp16_times(uint32_t a, uint32_t b) {
     return reinterpret_cast<const uint32_t&>(r);
 }
 
-// Eight codes times 2^(byte - 127) in bf16. fp16 holds a code's value with its exponent field in 14 .. 17 and at most one mantissa bit;
-// the same fields three bits further down are the value times 2^-112 in bf16.
-__device__ __forceinline__ uint4 to_bf16(uint32_t codes, uint32_t byte) {
-    const uint4 h = e2m1_values(codes);
-    uint32_t v[4] = {h.x, h.y, h.z, h.w};
-    const uint32_t one = byte == 255 ? 0x7FC0u : (min(byte, 142u) + 112) << 7;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = bf16_times((v[i] & 0x80008000u) | ((v[i] >> 3) & 0x0FFF0FFFu), one * 0x10001u);
-    if (byte > 142 && byte < 255) {   // scales above 2^15
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = bf16_times(v[i], ((byte - 142 + 127) << 7) * 0x10001u);
-    }
-    return make_uint4(v[0], v[1], v[2], v[3]);
-}
-// Eight codes times 2^(byte - top), byte <= top, in fp16.
-__device__ __forceinline__ uint4 to_fp16(uint32_t codes, uint32_t byte, uint32_t top) {
-    const uint4 h = e2m1_values(codes);
+// What 32 codes of a scale byte are multiplied with, in both halves of a word. bf16: the values come times 2^-112 (see to_values), so
+// 2^(byte - 15); scales above 2^15 need a second factor (bf16_more). fp16: 2^(byte - top), byte <= top. 255 is not a number.
+__device__ __forceinline__ uint32_t bf16_factor(uint32_t byte) { return (byte == 255 ? 0x7FC0u : (min(byte, 142u) + 112) << 7) * 0x10001u; }
+__device__ __forceinline__ uint32_t bf16_more(uint32_t byte) { return (byte > 142 && byte < 255 ? (byte - 142 + 127) << 7 : 0x3F80u) * 0x10001u; }
+__device__ __forceinline__ uint32_t fp16_factor(uint32_t byte, uint32_t top) {
     const uint32_t below = top - byte;
-    const uint32_t one = byte == 255 ? 0x7E00u : below < 15 ? (15 - below) << 10 : below < 25 ? 0x400u >> (below - 14) : 0u;
-    const uint32_t f = one * 0x10001u;
-    return make_uint4(fp16_times(h.x, f), fp16_times(h.y, f), fp16_times(h.z, f), fp16_times(h.w, f));
+    return (byte == 255 ? 0x7E00u : below < 15 ? (15 - below) << 10 : below < 25 ? 0x400u >> (below - 14) : 0u) * 0x10001u;
+}
+// Eight codes times a factor. fp16 holds a code's value with its exponent field in 14 .. 17 and at most one mantissa bit; for bf16 the same
+// fields three bits further down are the value times 2^-112.
+template <int DT>
+__device__ __forceinline__ uint4 to_values(uint32_t codes, uint32_t factor) {
+    uint4 h = e2m1_values(codes);
+    if constexpr (DT == ENEC_FP16) {
+        return make_uint4(fp16_times(h.x, factor), fp16_times(h.y, factor), fp16_times(h.z, factor), fp16_times(h.w, factor));
+    } else {
+        h.x = select_bits(0x80008000u, h.x, (h.x >> 3) & 0x0FFF0FFFu);
+        h.y = select_bits(0x80008000u, h.y, (h.y >> 3) & 0x0FFF0FFFu);
+        h.z = select_bits(0x80008000u, h.z, (h.z >> 3) & 0x0FFF0FFFu);
+        h.w = select_bits(0x80008000u, h.w, (h.w >> 3) & 0x0FFF0FFFu);
+        return make_uint4(bf16_times(h.x, factor), bf16_times(h.y, factor), bf16_times(h.z, factor), bf16_times(h.w, factor));
+    }
 }
 
 template <int DT, int MT>
@@ -256,6 +257,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const 
                 top[i] = most;
             }
         }
+        const uint32_t a_base = smem_u32(a_ring) + r * 128, shift = 8 * half;
+        uint32_t place[4];   // of the four chunks of eight values in the operand's row
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) place[e] = ((4 * half + e) ^ (r & 7)) << 4;
         bool ok = true;
         for (uint32_t k = 0; k < records && ok; ++k) {
             if (!suspended_wait(&raw_full, k & 1, &failed)) {
@@ -286,13 +291,21 @@ __global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const 
 #pragma unroll
                 for (uint32_t i = 0; i < MT; ++i) {
                     if (i >= mt) continue;
-                    const uint32_t word = q < 2 ? scales[i].x : scales[i].y;
-                    const uint32_t byte = word >> (8 * (2 * (q & 1) + half)) & 255;
-                    const uint32_t dst = smem_u32(a_ring) + (sa * MT + i) * 16384 + r * 128;
+                    const uint32_t byte = (q < 2 ? scales[i].x : scales[i].y) >> (16 * (q & 1) + shift) & 255;
+                    const uint32_t dst = a_base + (sa * MT + i) * 16384;
                     const uint32_t w[4] = {codes[i][q].x, codes[i][q].y, codes[i][q].z, codes[i][q].w};
+                    const uint32_t factor = DT == ENEC_BF16 ? bf16_factor(byte) : fp16_factor(byte, top[i]);
+                    if (DT == ENEC_BF16 && __any_sync(0xFFFFFFFFu, byte > 142 && byte < 255)) {
+                        const uint32_t more = bf16_more(byte);
 #pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e)
-                        sts128(dst + (((4 * half + e) ^ (r & 7)) << 4), DT == ENEC_BF16 ? to_bf16(w[e], byte) : to_fp16(w[e], byte, top[i]));
+                        for (uint32_t e = 0; e < 4; ++e) {
+                            const uint4 v = to_values<DT>(w[e], factor);
+                            sts128(dst + place[e], make_uint4(bf16_times(v.x, more), bf16_times(v.y, more), bf16_times(v.z, more), bf16_times(v.w, more)));
+                        }
+                    } else {
+#pragma unroll
+                        for (uint32_t e = 0; e < 4; ++e) sts128(dst + place[e], to_values<DT>(w[e], factor));
+                    }
                 }
                 fence_async_shared();
                 mbar_arrive(full_a + sa);
