@@ -1,9 +1,9 @@
 // y = x W^T for many tokens, W a microscaled stream, x of 16 bits: tcgen05.mma (kind::f16) on weights that are brought back on the way.
 //
 // Lanes of the accumulator are rows of W, its columns tokens: 256 (two accumulators) or 128 rows x up to 256 tokens a CTA. Of 64 columns
-// (a step) the tensor cores take 1024 clocks at 256 x 256. Meanwhile eight warps turn 16384 codes into 16-bit values in shared
-// memory (5 instructions a pair, some 370 clocks of the SM's issue slots) and eight warps fetch 32 KB of x with cp.async, 32 bytes a
-// clock from L2; tiles of 128 x 256 would need twice that, more than L2 gives to all SMs at a time. Raw records are copied in bulk; a
+// (a step) the tensor cores take 1024 clocks at 256 x 256. Meanwhile sixteen warps turn 16384 codes into 16-bit values in shared
+// memory (5 instructions a pair, some 370 clocks of the SM's issue slots), and 32 KB of x come by a tensor map, 32 bytes a clock from L2;
+// tiles of 128 x 256 would need twice that. Raw records are copied in bulk; a
 // thread takes its share of a record to registers at once, so that one record's room is enough.
 //
 // bf16: a code's value times its scale is exact in bf16 over the whole range of scales. fp16: it would not be, so a row's values are
@@ -14,15 +14,20 @@
 #include "enec_micro_mma.cuh"
 
 #include <cooperative_groups.h>
+#include <cuda.h>
+#include <cudaTypedefs.h>
 
 #include "enec_micro_launch.cuh"
 
 namespace enec {
 namespace {
 
-constexpr uint32_t kManyThreads = 18 * 32;   // bulk copies, matrix instructions, 8 warps for x, 8 for the weights and the results
+// Warps: bulk copies, matrix instructions, 8 for x, and 8 for each 128 rows of weights and results (half of them: 2048 x 4096 x 4096 took
+// 74 us, most of it the latency of bringing a step's weights back with two warps to a scheduler).
 constexpr uint32_t kFirstX = 2, kFirstW = 10, kThreadsX = 8 * 32;
-constexpr uint32_t kStagesA = 2, kStagesB = 3;
+template <int MT>
+__host__ __device__ constexpr uint32_t many_threads() { return (kFirstW + 8 * MT) * 32; }
+constexpr uint32_t kStagesA = 5, kStagesB = 3;   // of 128 rows x 64 columns of weights; of the tokens x 64 columns of x
 constexpr uint32_t kManyMostTokens = 256;
 
 struct ManyJob {
@@ -37,17 +42,21 @@ struct ManyJob {
     uint32_t row_tiles;      // tiles along the rows
     uint32_t cluster;        // CTAs that share a tile's columns
     uint32_t share;          // records of columns each takes
-    uint32_t aligned;        // rows of x begin on 16-byte boundaries
+    uint32_t aligned;        // rows of x begin on 16-byte boundaries: tiles of it come by the tensor map
+    CUtensorMap map;
     int* status;
 };
 
 template <int MT>
 __host__ __device__ constexpr uint32_t many_bytes(uint32_t tokens) {
-    return MT * kMicroRecordBytes + kStagesA * MT * 16384 + kStagesB * tokens * 128 + 1024;
+    return MT * kMicroRecordBytes + kStagesA * 16384 + kStagesB * tokens * 128 + 1024;
 }
 
-__device__ __forceinline__ void cp_async16_some(uint32_t dst, const void* src, uint32_t bytes) {   // the rest of the 16 are zeros
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+// 64 columns x tile_tokens rows of x from (column, token) on; zeros behind the matrix.
+__device__ __forceinline__ void tile_g2s(uint32_t dst, const CUtensorMap* map, uint32_t column, uint32_t token, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
+                 "r"(column), "r"(token), "r"(smem_u32(bar))
+                 : "memory");
 }
 
 __device__ __forceinline__ uint32_t bf16_times(uint32_t a, uint32_t b) {
@@ -84,7 +93,7 @@ __device__ __forceinline__ uint4 to_values(uint32_t codes, uint32_t factor) {
 }
 
 template <int DT, int MT>
-__global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const __grid_constant__ ManyJob job) {
+__global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(const __grid_constant__ ManyJob job) {
     extern __shared__ uint8_t raw_shared[];
     __shared__ uint64_t raw_full, raw_empty, full_a[kStagesA], empty_a[kStagesA], full_b[kStagesB], empty_b[kStagesB], done;
     __shared__ uint32_t tmem_at;
@@ -96,9 +105,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const 
     while (tmem_columns < MT * n) tmem_columns *= 2;
     if (threadIdx.x == 0) {
         mbar_init(&raw_full, 1);
-        mbar_init(&raw_empty, 256);
+        mbar_init(&raw_empty, 256 * MT);
         for (uint32_t i = 0; i < kStagesA; ++i) mbar_init(full_a + i, 256), mbar_init(empty_a + i, 1);
-        for (uint32_t i = 0; i < kStagesB; ++i) mbar_init(full_b + i, kThreadsX), mbar_init(empty_b + i, 1);
+        for (uint32_t i = 0; i < kStagesB; ++i) mbar_init(full_b + i, job.aligned ? 1 : kThreadsX), mbar_init(empty_b + i, 1);
         mbar_init(&done, 1);
         mbar_fence_init();
         failed = 0;
@@ -121,7 +130,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const 
     const uint64_t strip = uint64_t(job.s.col_tiles) * kMicroRecordBytes;
     const uint8_t* wr = job.w + kMicroHeaderBytes + row_tile * strip + uint64_t(k0) * kMicroRecordBytes;
     uint8_t* a_ring = smem;
-    uint8_t* b_ring = a_ring + kStagesA * MT * 16384;
+    uint8_t* b_ring = a_ring + kStagesA * 16384;
     uint8_t* raw = b_ring + kStagesB * n * 128;
     const bool good = micro_header_ok(job.w, job.s);
 
@@ -143,21 +152,25 @@ __global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const 
     } else if (warp == 1) {
         const uint32_t idesc = idesc_16bit(DT == ENEC_BF16, n);
         const uint64_t a0 = operand_desc(smem_u32(a_ring)), b0 = operand_desc(smem_u32(b_ring));
+        uint32_t slot = 0, phase = 0;
         for (uint32_t j = 0; j < steps; ++j) {
-            const uint32_t sa = j % kStagesA, sb = j % kStagesB;
-            if (!suspended_wait(full_a + sa, (j / kStagesA) & 1, &failed) || !suspended_wait(full_b + sb, (j / kStagesB) & 1, &failed)) {
+            const uint32_t sb = j % kStagesB;
+            bool there = suspended_wait(full_b + sb, (j / kStagesB) & 1, &failed);
+            const uint64_t b = b0 + sb * n * 8;
+            for (uint32_t i = 0; i < mt && there; ++i) {
+                there = suspended_wait(full_a + slot, phase, &failed);
+                if (!there) break;
+                tcgen05_fence_after();
+                const uint64_t a = a0 + slot * 1024;
+#pragma unroll
+                for (uint32_t q = 0; q < 4; ++q) mma_16bit(leader, tmem + i * n, a + q * 2, b + q * 2, idesc, j > 0 || q > 0);
+                tcgen05_commit(leader, empty_a + slot);
+                if (++slot == kStagesA) slot = 0, phase ^= 1;
+            }
+            if (!there) {
                 failed = 1;
                 break;
             }
-            tcgen05_fence_after();
-            const uint64_t a = a0 + sa * (MT * 1024), b = b0 + sb * n * 8;
-#pragma unroll
-            for (uint32_t i = 0; i < MT; ++i) {
-#pragma unroll
-                for (uint32_t q = 0; q < 4; ++q)
-                    mma_16bit(i < mt ? leader : 0, tmem + i * n, a + i * 1024 + q * 2, b + q * 2, idesc, j > 0 || q > 0);
-            }
-            tcgen05_commit(leader, empty_a + sa);
             tcgen05_commit(leader, empty_b + sb);
         }
         tcgen05_commit(leader, &done);
@@ -165,37 +178,25 @@ __global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const 
     } else if (warp < kFirstW) {
         // x: eight lanes a row of 64 columns
         const uint32_t me = threadIdx.x - kFirstX * 32, c = me & 7;
+        uint32_t asked = 0;
         const uint32_t first_col = min(k0 * kMicroCols, job.s.cols);
         const uint8_t* from = job.x + (uint64_t(token0) * job.ld_x + first_col) * 2;
         bool ok = true;
         if (job.aligned) {
-            for (uint32_t j = 0; j < steps; ++j) {
+            for (uint32_t j = 0; j < steps && warp == kFirstX; ++j) {
                 const uint32_t sb = j % kStagesB;
                 if (j >= kStagesB && !suspended_wait(empty_b + sb, (j / kStagesB - 1) & 1, &failed)) {
                     ok = false;
                     break;
                 }
-                const uint32_t dst = smem_u32(b_ring) + sb * n * 128;
-                const uint32_t col = j * 64 + c * 8;                                     // of this CTA's columns
-                const uint32_t valid = col < columns ? min(columns - col, 8u) : 0;
-                const uint8_t* here = from + (valid ? col : 0) * 2;
-#pragma unroll 4
-                for (uint32_t r = me >> 3; r < n; r += kThreadsX / 8) {
-                    const bool real = token0 + r < job.tokens;
-                    cp_async16_some(dst + r * 128 + ((c ^ (r & 7)) << 4), here + (real ? uint64_t(r) * job.ld_x * 2 : 0), real ? valid * 2 : 0);
+                if (leader) {
+                    mbar_expect_tx(full_b + sb, n * 128);
+                    tile_g2s(smem_u32(b_ring) + sb * n * 128, &job.map, first_col + j * 64, token0, full_b + sb);
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                if (j > 0) {   // the step before this one has arrived while this one is on its way
-                    asm volatile("cp.async.wait_group 1;" ::: "memory");
-                    fence_async_shared();
-                    mbar_arrive(full_b + (j - 1) % kStagesB);
-                }
+                asked = j + 1;
             }
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            if (ok && steps > 0) {
-                fence_async_shared();
-                mbar_arrive(full_b + (steps - 1) % kStagesB);
-            }
+            // nothing may be in flight when the CTA ends
+            for (uint32_t j = asked > kStagesB ? asked - kStagesB : 0; j < asked; ++j) mbar_wait_bounded(full_b + j % kStagesB, (j / kStagesB) & 1);
         } else {
             // rows that lie anywhere: through registers, 128 rows of a step at a time, the next ones' loads on the way meanwhile
             const uint32_t batches = (n + 127) / 128;
@@ -238,26 +239,24 @@ __global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const 
         }
         if (!ok) failed = 1;
     } else {
-        // the weights: thread (row, half) brings back 32 of the 64 columns of a step, of one row in each 128
-        const uint32_t me = threadIdx.x - kFirstW * 32, r = me & 127, half = me >> 7;
-        uint32_t top[MT];
+        // the weights: thread (tile, half, row) brings back 32 of the 64 columns of a step
+        const uint32_t me = threadIdx.x - kFirstW * 32, r = me & 127, half = me >> 7 & 1, i = me >> 8;
+        const bool mine = i < mt;   // the same for a warp
+        uint32_t top = 0;
         if constexpr (DT == ENEC_FP16) {
-#pragma unroll
-            for (uint32_t i = 0; i < MT; ++i) {
-                uint32_t most = 0;   // the largest of the row's scale bytes, four at a time; 255 does not count
-                const uint8_t* at = wr + i * strip + kMicroElemBytes + (r & 31) * 16 + (r >> 5) * 4;
-                if (i < mt) {
+            // the largest of the row's scale bytes, four at a time; 255 does not count
+            const uint8_t* at = wr + i * strip + kMicroElemBytes + (r & 31) * 16 + (r >> 5) * 4;
+            if (mine) {
 #pragma unroll 8
-                    for (uint32_t b = 0; b < 2 * records; ++b) {
-                        const uint32_t four = __ldg(reinterpret_cast<const uint32_t*>(at + uint64_t(b >> 1) * kMicroRecordBytes + (b & 1) * 512));
-                        most = __vmaxu4(most, four & ~__vcmpeq4(four, 0xFFFFFFFFu));
-                    }
+                for (uint32_t b = 0; b < 2 * records; ++b) {
+                    const uint32_t four = __ldg(reinterpret_cast<const uint32_t*>(at + uint64_t(b >> 1) * kMicroRecordBytes + (b & 1) * 512));
+                    top = __vmaxu4(top, four & ~__vcmpeq4(four, 0xFFFFFFFFu));
                 }
-                most = max(max(most & 255, most >> 8 & 255), max(most >> 16 & 255, most >> 24));
-                top[i] = most;
             }
+            top = max(max(top & 255, top >> 8 & 255), max(top >> 16 & 255, top >> 24));
         }
         const uint32_t a_base = smem_u32(a_ring) + r * 128, shift = 8 * half;
+        const uint32_t rec = smem_u32(raw) + i * kMicroRecordBytes;
         uint32_t place[4];   // of the four chunks of eight values in the operand's row
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e) place[e] = ((4 * half + e) ^ (r & 7)) << 4;
@@ -267,34 +266,29 @@ __global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const 
                 ok = false;
                 break;
             }
-            uint4 codes[MT][4];
-            uint2 scales[MT];   // eight bytes
+            uint4 codes[4];
+            uint2 scales = {};   // eight bytes
+            if (mine) {
 #pragma unroll
-            for (uint32_t i = 0; i < MT; ++i) {
-                if (i >= mt) continue;
-                const uint32_t rec = smem_u32(raw) + i * kMicroRecordBytes;
-#pragma unroll
-                for (uint32_t q = 0; q < 4; ++q) codes[i][q] = lds128(rec + r * 128 + (((2 * q + half) ^ (r & 7)) << 4));
+                for (uint32_t q = 0; q < 4; ++q) codes[q] = lds128(rec + r * 128 + (((2 * q + half) ^ (r & 7)) << 4));
                 const uint32_t at = rec + kMicroElemBytes + (r & 31) * 16 + (r >> 5) * 4;
-                scales[i] = make_uint2(lds32(at), lds32(at + 512));
+                scales = make_uint2(lds32(at), lds32(at + 512));
             }
             mbar_arrive(&raw_empty);
             const uint32_t here = min(4u, steps - 4 * k);
 #pragma unroll
             for (uint32_t q = 0; q < 4; ++q) {
                 if (q >= here) break;
-                const uint32_t j = 4 * k + q, sa = j % kStagesA;
-                if (j >= kStagesA && !suspended_wait(empty_a + sa, (j / kStagesA - 1) & 1, &failed)) {
-                    ok = false;
-                    break;
-                }
-#pragma unroll
-                for (uint32_t i = 0; i < MT; ++i) {
-                    if (i >= mt) continue;
-                    const uint32_t byte = (q < 2 ? scales[i].x : scales[i].y) >> (16 * (q & 1) + shift) & 255;
-                    const uint32_t dst = a_base + (sa * MT + i) * 16384;
-                    const uint32_t w[4] = {codes[i][q].x, codes[i][q].y, codes[i][q].z, codes[i][q].w};
-                    const uint32_t factor = DT == ENEC_BF16 ? bf16_factor(byte) : fp16_factor(byte, top[i]);
+                if (mine) {
+                    const uint32_t use = (4 * k + q) * mt + i, sa = use % kStagesA;
+                    if (use >= kStagesA && !suspended_wait(empty_a + sa, (use / kStagesA - 1) & 1, &failed)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t byte = (q < 2 ? scales.x : scales.y) >> (16 * (q & 1) + shift) & 255;
+                    const uint32_t dst = a_base + sa * 16384;
+                    const uint32_t w[4] = {codes[q].x, codes[q].y, codes[q].z, codes[q].w};
+                    const uint32_t factor = DT == ENEC_BF16 ? bf16_factor(byte) : fp16_factor(byte, top);
                     if (DT == ENEC_BF16 && __any_sync(0xFFFFFFFFu, byte > 142 && byte < 255)) {
                         const uint32_t more = bf16_more(byte);
 #pragma unroll
@@ -306,47 +300,38 @@ __global__ void __launch_bounds__(kManyThreads, 1) enec_micro_many_kernel(const 
 #pragma unroll
                         for (uint32_t e = 0; e < 4; ++e) sts128(dst + place[e], to_values<DT>(w[e], factor));
                     }
+                    fence_async_shared();
+                    mbar_arrive(full_a + sa);
                 }
-                fence_async_shared();
-                mbar_arrive(full_a + sa);
             }
         }
         if (!ok) failed = 1;
         if (!suspended_wait(&done, 0, &failed)) failed = 1;
         tcgen05_fence_after();
-        // results: the warp's quarter of the lanes, every other 16 tokens
-        const uint32_t quarter = warp & 3, group = (warp - kFirstW) >> 2;
-        const uint32_t row_in = quarter * 32 + lane;
-        float factor[MT];
-#pragma unroll
-        for (uint32_t i = 0; i < MT; ++i) factor[i] = 1.f;
+        // results: the warp's quarter of the lanes, every other 16 tokens of its tile
+        const uint32_t quarter = warp & 3, row_in = quarter * 32 + lane, row = (row_tile + i) * kMicroRows + row_in;
+        float factor = 1.f;
         if constexpr (DT == ENEC_FP16) {
             // the rows' exponents change hands through shared memory that no operand uses any more
             uint8_t* tops = smem;
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-#pragma unroll
-            for (uint32_t i = 0; i < MT; ++i)
-                if (half == 0) tops[i * 128 + r] = uint8_t(top[i]);
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-#pragma unroll
-            for (uint32_t i = 0; i < MT; ++i) factor[i] = micro_scale(tops[i * 128 + row_in]);
-            asm volatile("bar.sync 1, 256;" ::: "memory");
+            asm volatile("bar.sync 1, %0;" ::"n"(256 * MT) : "memory");
+            if (half == 0) tops[i * 128 + r] = uint8_t(top);
+            asm volatile("bar.sync 1, %0;" ::"n"(256 * MT) : "memory");
+            factor = micro_scale(tops[i * 128 + row_in]);
+            asm volatile("bar.sync 1, %0;" ::"n"(256 * MT) : "memory");
         }
-        if (!failed && steps > 0) {
-            for (uint32_t i = 0; i < mt; ++i) {
-                const uint32_t row = (row_tile + i) * kMicroRows + row_in;
-                for (uint32_t c = group * 16; c < n; c += 32) {
-                    if (token0 + c >= job.tokens) break;
-                    uint32_t v[16];
-                    tmem_load16(tmem + (quarter * 32 << 16) + i * n + c, v);
-                    tmem_load_wait();
-                    if (MT == 1 && job.cluster > 1) {
-                        float* sums = reinterpret_cast<float*>(smem);   // [token][row]
+        if (!failed && steps > 0 && mine) {
+            for (uint32_t c = half * 16; c < n; c += 32) {
+                if (token0 + c >= job.tokens) break;
+                uint32_t v[16];
+                tmem_load16(tmem + (quarter * 32 << 16) + i * n + c, v);
+                tmem_load_wait();
+                if (MT == 1 && job.cluster > 1) {
+                    float* sums = reinterpret_cast<float*>(smem);   // [token][row]
 #pragma unroll
-                        for (uint32_t e = 0; e < 16; ++e) sums[(c + e) * kMicroRows + row_in] = __uint_as_float(v[e]) * factor[i];
-                    } else if (good) {
-                        store_tile16<DT>(job.y, job.ld_y, token0 + c, job.tokens, row, job.s.rows, v, factor[i], lane);
-                    }
+                    for (uint32_t e = 0; e < 16; ++e) sums[(c + e) * kMicroRows + row_in] = __uint_as_float(v[e]) * factor;
+                } else if (good) {
+                    store_tile16<DT>(job.y, job.ld_y, token0 + c, job.tokens, row, job.s.rows, v, factor, lane);
                 }
             }
         }
@@ -387,7 +372,7 @@ enec_status launch_many(const ManyJob& job, uint32_t tiles, const MicroDevice& d
     if (!allow_shared(allowed, dev, enec_micro_many_kernel<DT, MT>, many_bytes<MT>(kManyMostTokens))) return ENEC_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(tiles * job.cluster);
-    cfg.blockDim = dim3(kManyThreads);
+    cfg.blockDim = dim3(many_threads<MT>());
     cfg.dynamicSmemBytes = many_bytes<MT>(job.tile_tokens);
     if (job.cluster > 1 && cfg.dynamicSmemBytes < job.tile_tokens * kMicroRows * 4 + 1024) cfg.dynamicSmemBytes = job.tile_tokens * kMicroRows * 4 + 1024;
     const uint32_t least = MT * job.tile_tokens > 256 ? kTmemAloneShared : kTmemHalfShared;
@@ -408,6 +393,19 @@ enec_status launch_many(const ManyJob& job, uint32_t tiles, const MicroDevice& d
 
 }  // namespace
 
+// The driver's encoder of tensor maps, found once; null where there is none.
+PFN_cuTensorMapEncodeTiled_v12000 map_encoder() {
+    static const PFN_cuTensorMapEncodeTiled_v12000 encode = []() -> PFN_cuTensorMapEncodeTiled_v12000 {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return nullptr;
+        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+    }();
+    return encode;
+}
+
 enec_status micro_many(const MicroProduct& p, const MicroDevice& dev, cudaStream_t stream) {
     ManyJob job;
     job.x = p.x;
@@ -417,10 +415,20 @@ enec_status micro_many(const MicroProduct& p, const MicroDevice& dev, cudaStream
     job.y = p.y;
     job.ld_y = p.ld_y;
     job.tokens = p.tokens;
-    job.aligned = p.ld_x % 8 == 0;
     job.status = p.status;
     const uint64_t token_tiles = (p.tokens + kManyMostTokens - 1) / kManyMostTokens;
     job.tile_tokens = uint32_t(((p.tokens + token_tiles - 1) / token_tiles + 15) / 16 * 16);
+    // a map's stride is a multiple of 16 bytes and below 2^40
+    job.aligned = p.ld_x % 8 == 0;
+    if (job.aligned) {
+        const cuuint64_t extent[2] = {p.s.cols, p.tokens}, stride[1] = {p.ld_x * 2};
+        const cuuint32_t box[2] = {64, job.tile_tokens}, step[2] = {1, 1};
+        const auto encode = map_encoder();
+        if (!encode || encode(&job.map, p.dt == ENEC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                              const_cast<uint8_t*>(p.x), extent, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return ENEC_ERR_CUDA;
+    }
     // 256 rows a tile where that leaves work for most SMs; else 128, and the columns shared out while more than one tile an SM is missing
     uint32_t mt = 2;
     uint64_t tiles = (p.s.row_tiles + 1) / 2 * token_tiles;
