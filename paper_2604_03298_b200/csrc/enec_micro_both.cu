@@ -13,7 +13,7 @@
 namespace enec {
 namespace {
 
-constexpr uint32_t kBothStages = 3;
+constexpr uint32_t kBothMostStages = 8;
 constexpr uint32_t kBothThreads = 320;       // copies, matrix instructions, eight warps that store
 constexpr uint32_t kBothMostTokens = 192;    // of a tile
 constexpr uint32_t kScaleColumns = 32;       // of a stage in tensor memory: 8 for each 128 rows of W, 16 for the tokens
@@ -26,6 +26,7 @@ struct BothJob {
     uint64_t ld_y;
     uint32_t tile_tokens;
     uint32_t row_tiles;      // tiles along the rows of W
+    uint32_t stages;
     int* status;
 };
 
@@ -35,14 +36,14 @@ __host__ __device__ constexpr uint32_t both_stage_bytes(uint32_t tokens) { retur
 template <int DT, int MT>
 __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const __grid_constant__ BothJob job) {
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t full[kBothStages], empty[kBothStages], done;
+    __shared__ uint64_t full[kBothMostStages], empty[kBothMostStages], done;
     __shared__ uint32_t tmem_at;
     __shared__ volatile int failed;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     const uint32_t n = job.tile_tokens, stage_bytes = both_stage_bytes<MT>(n);
     if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < kBothStages; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
+        for (uint32_t i = 0; i < job.stages; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
         mbar_init(&done, 1);
         mbar_fence_init();
         failed = 0;
@@ -69,10 +70,9 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
     const uint32_t leader = elected();
     if (warp == 0) {
         const uint32_t bytes = mt * kMicroRecordBytes + first_rows * 128 + 1024 + (second ? (n - first_rows) * 128 + 1024 : 0);
-        uint32_t k = 0;
+        uint32_t k = 0, s = 0, phase = 1;
         for (; k < records; ++k) {
-            const uint32_t s = k % kBothStages;
-            if (k >= kBothStages && !suspended_wait(empty + s, (k / kBothStages - 1) & 1, &failed)) {
+            if (k >= job.stages && !suspended_wait(empty + s, phase, &failed)) {
                 failed = 1;
                 break;
             }
@@ -93,15 +93,16 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
                     bulk_g2s(scales + MT * 1024 + 1024, xr + strip + at + kMicroElemBytes, 1024, full + s);
                 }
             }
+            if (++s == job.stages) s = 0, phase ^= 1;
         }
         // nothing may be in flight when the CTA ends
-        for (uint32_t i = k > kBothStages ? k - kBothStages : 0; i < k; ++i) mbar_wait_bounded(full + i % kBothStages, (i / kBothStages) & 1);
+        for (uint32_t i = k > job.stages ? k - job.stages : 0; i < k; ++i) mbar_wait_bounded(full + i % job.stages, (i / job.stages) & 1);
     } else if (warp == 1) {
         const uint32_t idesc = scaled_idesc(n);
         const uint64_t operands = operand_desc(smem_u32(smem)), scales = scale_desc(smem_u32(smem) + MT * kMicroElemBytes + n * 128);
+        uint32_t s = 0, phase = 0;
         for (uint32_t k = 0; k < records; ++k) {
-            const uint32_t s = k % kBothStages;
-            if (!suspended_wait(full + s, (k / kBothStages) & 1, &failed)) {
+            if (!suspended_wait(full + s, phase, &failed)) {
                 failed = 1;
                 break;
             }
@@ -127,6 +128,7 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
                                idesc | pair << 4 | pair << 29, to + (2 * i + h) * 4, scale_x, k > 0 || q > 0);
             }
             tcgen05_commit(leader, empty + s);
+            if (++s == job.stages) s = 0, phase ^= 1;
         }
         tcgen05_commit(leader, &done);
         mbar_wait_bounded(&done, 0);   // no instruction may be under way when tensor memory is given back
@@ -157,11 +159,14 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
 }
 
 template <int DT, int MT>
-enec_status launch_both(const BothJob& job, uint32_t grid, const MicroDevice& dev, cudaStream_t stream) {
+enec_status launch_both(BothJob job, uint32_t grid, const MicroDevice& dev, cudaStream_t stream) {
     static std::atomic<uint64_t> allowed{0};
-    constexpr uint32_t most = kBothStages * both_stage_bytes<MT>(kBothMostTokens) + 1024;
-    if (!allow_shared(allowed, dev, enec_micro_both_kernel<DT, MT>, most < kTmemAloneShared ? kTmemAloneShared : most)) return ENEC_ERR_CUDA;
-    uint32_t bytes = kBothStages * both_stage_bytes<MT>(job.tile_tokens) + 1024;
+    if (!allow_shared(allowed, dev, enec_micro_both_kernel<DT, MT>, kFewMostShared)) return ENEC_ERR_CUDA;
+    // as many stages as fit into shared memory, and their scales beside the sums in tensor memory: three of the largest tile
+    const uint32_t fit = (kFewMostShared - 1024) / both_stage_bytes<MT>(job.tile_tokens), columns = (512 - MT * kBothMostTokens) / kScaleColumns;
+    job.stages = fit < columns ? fit : columns;
+    if (job.stages > kBothMostStages) job.stages = kBothMostStages;
+    uint32_t bytes = job.stages * both_stage_bytes<MT>(job.tile_tokens) + 1024;
     if (bytes < kTmemAloneShared) bytes = kTmemAloneShared;
     const cudaError_t err = launch_pdl(enec_micro_both_kernel<DT, MT>, grid, kBothThreads, bytes, stream, job);
     g_launches.fetch_add(1, std::memory_order_relaxed);

@@ -47,9 +47,13 @@ struct ManyJob {
     int* status;
 };
 
+// Records of raw weights on the way or in use: one where shared memory is short, two where it is not and latency counts.
+template <int MT>
+__host__ __device__ constexpr uint32_t raw_stages() { return MT == 1 ? 2 : 1; }
+
 template <int MT>
 __host__ __device__ constexpr uint32_t many_bytes(uint32_t tokens) {
-    return MT * kMicroRecordBytes + kStagesA * 16384 + kStagesB * tokens * 128 + 1024;
+    return raw_stages<MT>() * MT * kMicroRecordBytes + kStagesA * 16384 + kStagesB * tokens * 128 + 1024;
 }
 
 // 64 columns x tile_tokens rows of x from (column, token) on; zeros behind the matrix.
@@ -95,7 +99,8 @@ __device__ __forceinline__ uint4 to_values(uint32_t codes, uint32_t factor) {
 template <int DT, int MT>
 __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(const __grid_constant__ ManyJob job) {
     extern __shared__ uint8_t raw_shared[];
-    __shared__ uint64_t raw_full, raw_empty, full_a[kStagesA], empty_a[kStagesA], full_b[kStagesB], empty_b[kStagesB], done;
+    constexpr uint32_t kRaw = raw_stages<MT>();
+    __shared__ uint64_t raw_full[raw_stages<MT>()], raw_empty[raw_stages<MT>()], full_a[kStagesA], empty_a[kStagesA], full_b[kStagesB], empty_b[kStagesB], done;
     __shared__ uint32_t tmem_at;
     __shared__ volatile int failed;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -104,8 +109,7 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
     uint32_t tmem_columns = 32;
     while (tmem_columns < MT * n) tmem_columns *= 2;
     if (threadIdx.x == 0) {
-        mbar_init(&raw_full, 1);
-        mbar_init(&raw_empty, 256 * MT);
+        for (uint32_t i = 0; i < kRaw; ++i) mbar_init(raw_full + i, 1), mbar_init(raw_empty + i, 256 * MT);
         for (uint32_t i = 0; i < kStagesA; ++i) mbar_init(full_a + i, 256), mbar_init(empty_a + i, 1);
         for (uint32_t i = 0; i < kStagesB; ++i) mbar_init(full_b + i, job.aligned ? 1 : kThreadsX), mbar_init(empty_b + i, 1);
         mbar_init(&done, 1);
@@ -138,17 +142,19 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
     if (warp == 0) {
         uint32_t k = 0;
         for (; k < records; ++k) {
-            if (k > 0 && !suspended_wait(&raw_empty, (k - 1) & 1, &failed)) {
+            const uint32_t s = k % kRaw;
+            if (k >= kRaw && !suspended_wait(raw_empty + s, (k / kRaw - 1) & 1, &failed)) {
                 failed = 1;
                 break;
             }
             if (leader) {
-                mbar_expect_tx(&raw_full, mt * kMicroRecordBytes);
+                mbar_expect_tx(raw_full + s, mt * kMicroRecordBytes);
                 for (uint32_t i = 0; i < mt; ++i)
-                    bulk_g2s(raw + i * kMicroRecordBytes, wr + i * strip + uint64_t(k) * kMicroRecordBytes, kMicroRecordBytes, &raw_full);
+                    bulk_g2s(raw + (s * MT + i) * kMicroRecordBytes, wr + i * strip + uint64_t(k) * kMicroRecordBytes, kMicroRecordBytes, raw_full + s);
             }
         }
-        if (k > 0) mbar_wait_bounded(&raw_full, (k - 1) & 1);   // nothing may be in flight when the CTA ends
+        // nothing may be in flight when the CTA ends
+        for (uint32_t i = k > kRaw ? k - kRaw : 0; i < k; ++i) mbar_wait_bounded(raw_full + i % kRaw, (i / kRaw) & 1);
     } else if (warp == 1) {
         const uint32_t idesc = idesc_16bit(DT == ENEC_BF16, n);
         const uint64_t a0 = operand_desc(smem_u32(a_ring)), b0 = operand_desc(smem_u32(b_ring));
@@ -198,43 +204,41 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
             // nothing may be in flight when the CTA ends
             for (uint32_t j = asked > kStagesB ? asked - kStagesB : 0; j < asked; ++j) mbar_wait_bounded(full_b + j % kStagesB, (j / kStagesB) & 1);
         } else {
-            // rows that lie anywhere: through registers, 128 rows of a step at a time, the next ones' loads on the way meanwhile
-            const uint32_t batches = (n + 127) / 128;
-            uint32_t next[4][4];
-            auto load = [&](uint32_t j, uint32_t batch) {
-                const uint32_t col = j * 64 + c * 8;
-                const int valid = col < columns ? int(min(columns - col, 8u)) : 0;
+            // rows that lie anywhere: through registers, 64 rows of a step at a time, the loads of four such batches on the way together
+            constexpr uint32_t kAhead = 4;
+            const uint32_t batches = (n + 63) / 64, all = steps * batches;
+            uint32_t v[kAhead][2][4];
+            auto load = [&](uint32_t (*to)[4], uint32_t batch) {
+                const uint32_t j = batch / batches, col = j * 64 + c * 8, first = (batch - j * batches) * 64;
+                const int valid = batch < all && col < columns ? int(min(columns - col, 8u)) : 0;
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t r = batch * 128 + i * 32 + (me >> 3);
-                    load_eight<DT>(from + (uint64_t(r) * job.ld_x + col) * 2, r < n && token0 + r < job.tokens ? valid : 0, next[i]);
+                for (uint32_t i = 0; i < 2; ++i) {
+                    const uint32_t r = first + i * 32 + (me >> 3);
+                    load_eight<DT>(from + (uint64_t(r) * job.ld_x + col) * 2, r < n && token0 + r < job.tokens ? valid : 0, to[i]);
                 }
             };
-            if (steps > 0) load(0, 0);
-            for (uint32_t j = 0; j < steps && ok; ++j) {
-                const uint32_t sb = j % kStagesB, dst = smem_u32(b_ring) + sb * n * 128;
-                for (uint32_t batch = 0; batch < batches; ++batch) {
-                    uint32_t v[4][4];
 #pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i) {
+            for (uint32_t a = 0; a < kAhead; ++a) load(v[a], a);
+            for (uint32_t batch0 = 0; batch0 < all && ok; batch0 += kAhead) {
 #pragma unroll
-                        for (uint32_t e = 0; e < 4; ++e) v[i][e] = next[i][e];
-                    }
-                    if (batch + 1 < batches) load(j, batch + 1);
-                    else if (j + 1 < steps) load(j + 1, 0);
-                    if (batch == 0 && j >= kStagesB && !suspended_wait(empty_b + sb, (j / kStagesB - 1) & 1, &failed)) {
+                for (uint32_t a = 0; a < kAhead; ++a) {
+                    const uint32_t batch = batch0 + a, j = batch / batches, part = batch - j * batches, sb = j % kStagesB;
+                    if (batch >= all || !ok) break;
+                    if (part == 0 && j >= kStagesB && !suspended_wait(empty_b + sb, (j / kStagesB - 1) & 1, &failed)) {
                         ok = false;
                         break;
                     }
 #pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i) {
-                        const uint32_t r = batch * 128 + i * 32 + (me >> 3);
-                        if (r < n) sts128(dst + r * 128 + ((c ^ (r & 7)) << 4), make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]));
+                    for (uint32_t i = 0; i < 2; ++i) {
+                        const uint32_t r = part * 64 + i * 32 + (me >> 3);
+                        if (r < n) sts128(smem_u32(b_ring) + sb * n * 128 + r * 128 + ((c ^ (r & 7)) << 4), make_uint4(v[a][i][0], v[a][i][1], v[a][i][2], v[a][i][3]));
+                    }
+                    load(v[a], batch + kAhead);
+                    if (part == batches - 1) {
+                        fence_async_shared();
+                        mbar_arrive(full_b + sb);
                     }
                 }
-                if (!ok) break;
-                fence_async_shared();
-                mbar_arrive(full_b + sb);
             }
         }
         if (!ok) failed = 1;
@@ -256,25 +260,25 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
             top = max(max(top & 255, top >> 8 & 255), max(top >> 16 & 255, top >> 24));
         }
         const uint32_t a_base = smem_u32(a_ring) + r * 128, shift = 8 * half;
-        const uint32_t rec = smem_u32(raw) + i * kMicroRecordBytes;
         uint32_t place[4];   // of the four chunks of eight values in the operand's row
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e) place[e] = ((4 * half + e) ^ (r & 7)) << 4;
         bool ok = true;
         for (uint32_t k = 0; k < records && ok; ++k) {
-            if (!suspended_wait(&raw_full, k & 1, &failed)) {
+            if (!suspended_wait(raw_full + k % kRaw, (k / kRaw) & 1, &failed)) {
                 ok = false;
                 break;
             }
             uint4 codes[4];
             uint2 scales = {};   // eight bytes
+            const uint32_t rec = smem_u32(raw) + (k % kRaw * MT + i) * kMicroRecordBytes;
             if (mine) {
 #pragma unroll
                 for (uint32_t q = 0; q < 4; ++q) codes[q] = lds128(rec + r * 128 + (((2 * q + half) ^ (r & 7)) << 4));
                 const uint32_t at = rec + kMicroElemBytes + (r & 31) * 16 + (r >> 5) * 4;
                 scales = make_uint2(lds32(at), lds32(at + 512));
             }
-            mbar_arrive(&raw_empty);
+            mbar_arrive(raw_empty + k % kRaw);
             const uint32_t here = min(4u, steps - 4 * k);
 #pragma unroll
             for (uint32_t q = 0; q < 4; ++q) {
