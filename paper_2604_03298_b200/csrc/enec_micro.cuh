@@ -131,17 +131,55 @@ struct MicroType<ENEC_FP32> {
     static __device__ __forceinline__ T one(float a) { return a; }
 };
 
-// Eight neighbouring elements (16 or 32 bytes) as words, zeros behind the first `valid`. p lies on a multiple of the element
-// size only; the loads are of the 16-byte granules that hold the elements, and none is of a granule without one.
+// Eight neighbouring elements (16 or 32 bytes) from anywhere on a multiple of the element size: the 16-byte granules that hold them (one
+// more than aligned ones would need; none is read that holds no element), to be shifted into words when they are needed.
+template <int DT>
+struct EightLoaded {
+    static constexpr int kElem = DT == ENEC_FP32 ? 4 : 2;
+    static constexpr int kWords = 2 * kElem;
+    uint32_t a[kWords + 4];
+    uint32_t off;
+    int valid;   // elements, the first ones; 8 and more: all
+    __device__ __forceinline__ void load(const uint8_t* p, int valid_) {
+        valid = valid_;
+        off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15u;
+        const uint8_t* base = p - off;
+        const int last = valid > 0 ? int(off) + min(valid, 8) * kElem : 0;   // bytes from base to the end of the elements
+#pragma unroll
+        for (int g = 0; g < kWords / 4 + 1; ++g) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (16 * g < last) v = __ldg(reinterpret_cast<const uint4*>(base + 16 * g));
+            a[4 * g] = v.x, a[4 * g + 1] = v.y, a[4 * g + 2] = v.z, a[4 * g + 3] = v.w;
+        }
+    }
+    // The elements as words, zeros behind the valid ones.
+    __device__ __forceinline__ void words(uint32_t* w) {
+        if (off & 8) {
+#pragma unroll
+            for (int i = 0; i < kWords + 2; ++i) a[i] = a[i + 2];
+        }
+        if (off & 4) {
+#pragma unroll
+            for (int i = 0; i < kWords + 1; ++i) a[i] = a[i + 1];
+        }
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = off & 2 ? __funnelshift_r(a[i], a[i + 1], 16) : a[i];
+        if (valid < 8) {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+                if (kElem == 4) w[i] = i < valid ? w[i] : 0;
+                if (kElem == 2) w[i] = 2 * i + 1 < valid ? w[i] : 2 * i < valid ? w[i] & 0xFFFFu : 0;
+            }
+        }
+    }
+};
 template <int DT>
 __device__ __forceinline__ void load_eight(const uint8_t* p, int valid, uint32_t* w) {
-    constexpr int kElem = DT == ENEC_FP32 ? 4 : 2;
-    constexpr int kWords = 2 * kElem;
+    constexpr int kWords = EightLoaded<DT>::kWords;
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = 0;
     if (valid <= 0) return;
-    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15u;
-    if (off == 0 && valid == 8) {
+    if ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && valid >= 8) {
 #pragma unroll
         for (int g = 0; g < kWords / 4; ++g) {
             const uint4 v = __ldg(reinterpret_cast<const uint4*>(p + 16 * g));
@@ -149,32 +187,9 @@ __device__ __forceinline__ void load_eight(const uint8_t* p, int valid, uint32_t
         }
         return;
     }
-    const uint8_t* base = p - off;
-    const int last = int(off) + valid * kElem;   // bytes from base to the end of the elements
-    uint32_t a[kWords + 4];
-#pragma unroll
-    for (int g = 0; g < kWords / 4 + 1; ++g) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (16 * g < last) v = __ldg(reinterpret_cast<const uint4*>(base + 16 * g));
-        a[4 * g] = v.x, a[4 * g + 1] = v.y, a[4 * g + 2] = v.z, a[4 * g + 3] = v.w;
-    }
-    if (off & 8) {
-#pragma unroll
-        for (int i = 0; i < kWords + 2; ++i) a[i] = a[i + 2];
-    }
-    if (off & 4) {
-#pragma unroll
-        for (int i = 0; i < kWords + 1; ++i) a[i] = a[i + 1];
-    }
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = off & 2 ? __funnelshift_r(a[i], a[i + 1], 16) : a[i];
-    if (valid < 8) {
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-            if (kElem == 4) w[i] = i < valid ? w[i] : 0;
-            if (kElem == 2) w[i] = 2 * i + 1 < valid ? w[i] : 2 * i < valid ? w[i] & 0xFFFFu : 0;
-        }
-    }
+    EightLoaded<DT> eight;
+    eight.load(p, valid);
+    eight.words(w);
 }
 
 template <int DT>

@@ -204,17 +204,17 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
             // nothing may be in flight when the CTA ends
             for (uint32_t j = asked > kStagesB ? asked - kStagesB : 0; j < asked; ++j) mbar_wait_bounded(full_b + j % kStagesB, (j / kStagesB) & 1);
         } else {
-            // rows that lie anywhere: through registers, 64 rows of a step at a time, the loads of four such batches on the way together
-            constexpr uint32_t kAhead = 4;
+            // rows that lie anywhere: through registers, 64 rows of a step at a time, the loads of three such batches on the way together
+            constexpr uint32_t kAhead = 3;
             const uint32_t batches = (n + 63) / 64, all = steps * batches;
-            uint32_t v[kAhead][2][4];
-            auto load = [&](uint32_t (*to)[4], uint32_t batch) {
+            EightLoaded<DT> v[kAhead][2];
+            auto load = [&](EightLoaded<DT>* to, uint32_t batch) {
                 const uint32_t j = batch / batches, col = j * 64 + c * 8, first = (batch - j * batches) * 64;
                 const int valid = batch < all && col < columns ? int(min(columns - col, 8u)) : 0;
 #pragma unroll
                 for (uint32_t i = 0; i < 2; ++i) {
                     const uint32_t r = first + i * 32 + (me >> 3);
-                    load_eight<DT>(from + (uint64_t(r) * job.ld_x + col) * 2, r < n && token0 + r < job.tokens ? valid : 0, to[i]);
+                    to[i].load(from + (uint64_t(r) * job.ld_x + col) * 2, r < n && token0 + r < job.tokens ? valid : 0);
                 }
             };
 #pragma unroll
@@ -231,7 +231,9 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
 #pragma unroll
                     for (uint32_t i = 0; i < 2; ++i) {
                         const uint32_t r = part * 64 + i * 32 + (me >> 3);
-                        if (r < n) sts128(smem_u32(b_ring) + sb * n * 128 + r * 128 + ((c ^ (r & 7)) << 4), make_uint4(v[a][i][0], v[a][i][1], v[a][i][2], v[a][i][3]));
+                        uint32_t w[4];
+                        v[a][i].words(w);
+                        if (r < n) sts128(smem_u32(b_ring) + sb * n * 128 + r * 128 + ((c ^ (r & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
                     }
                     load(v[a], batch + kAhead);
                     if (part == batches - 1) {
@@ -358,10 +360,12 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
             const uint32_t row_in = threadIdx.x & 127;
             const uint32_t row = row_tile * kMicroRows + row_in;
             if (threadIdx.x < 512 && good && !failed && row < job.s.rows) {
+#pragma unroll 2
                 for (uint32_t t = (threadIdx.x >> 7) * job.cluster + rank; t < n && token0 + t < job.tokens; t += 4 * job.cluster) {
                     float v = 0.f;
-                    for (uint32_t k = 0; k < with; ++k)
-                        v += cluster.map_shared_rank(reinterpret_cast<float*>(smem), k)[t * kMicroRows + row_in];
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k)
+                        if (k < with) v += cluster.map_shared_rank(reinterpret_cast<float*>(smem), k)[t * kMicroRows + row_in];
                     reinterpret_cast<T*>(job.y)[uint64_t(token0 + t) * job.ld_y + row] = MicroType<DT>::one(v);
                 }
             }
