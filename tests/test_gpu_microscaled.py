@@ -239,7 +239,7 @@ def test_repeated_captured_and_concurrent_calls_agree_bit_for_bit(tokens):
         assert E.enec_matmul_microscaled(x, 0, tokens, 1000, stream, stream.numel(), 300, 1000, y, 300) == 0
     call(ys[0])
     torch.cuda.synchronize()
-    side = [torch.cuda.Stream() for _ in range(2)]
+    side = [torch.cuda.Stream(priority=-1) for _ in range(2)]
     for s, y in zip(side, ys[1:3]):
         s.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(s):

@@ -95,7 +95,7 @@ def test_quantised_activations_through_the_product_captured_and_on_two_streams()
     call(ys[0], xss[0])
     torch.cuda.synchronize()
     for i in (1, 2):
-        s = torch.cuda.Stream()
+        s = torch.cuda.Stream(priority=-1)
         with torch.cuda.stream(s):
             call(ys[i], xss[i])
     torch.cuda.synchronize()

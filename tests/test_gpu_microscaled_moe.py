@@ -202,7 +202,7 @@ def test_repeated_captured_and_concurrent_calls_agree_bit_for_bit(tokens):
     run(0)
     torch.cuda.synchronize()
     for i in (1, 2):
-        s = torch.cuda.Stream()
+        s = torch.cuda.Stream(priority=-1)
         with torch.cuda.stream(s):
             run(i)
     torch.cuda.synchronize()
