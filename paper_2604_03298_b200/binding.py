@@ -95,9 +95,13 @@ def lib():
     return _LIB
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream   # of a device, an integer
+_device = torch.cuda.current_device
+
+
 def _stream():
     # raw handle of torch's current stream on the current device (an integer; 0 is the legacy default stream)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _ptr(t):
@@ -183,42 +187,57 @@ def enec_compress_batched(items, dt, d_out_sizes=None, d_status=None) -> int:
                                        _stream())
 
 
+# The microscaled calls of one token take a few microseconds on the GPU, so what Python adds counts: entry points are looked up once.
+class _Micro:
+    def __getattr__(self, name):     # the first use of an entry point; later ones find it in the instance
+        f = getattr(lib(), name)
+        setattr(self, name, f)
+        return f
+
+
+_micro = _Micro()
+
+
 def enec_microscaled_size(batch: int, rows: int, cols: int) -> int:
     """Bytes of a microscaled 4-bit stream of `batch` matrices of rows x cols values."""
-    return lib().enec_microscaled_size(batch, rows, cols)
+    return _micro.enec_microscaled_size(batch, rows, cols)
 
 
 def enec_quantize_microscaled(d_in, dt, batch, rows, cols, ld, d_out, out_capacity, d_status=None) -> int:
     """[batch, rows, cols] values, rows `ld` values apart, into the microscaled stream d_out."""
-    return lib().enec_quantize_microscaled(_ptr(d_in), dt, batch, rows, cols, ld, _ptr(d_out), out_capacity, _ptr(d_status), _stream())
+    return _micro.enec_quantize_microscaled(None if d_in is None else d_in.data_ptr(), dt, batch, rows, cols, ld, d_out.data_ptr(), out_capacity,
+                                            None if d_status is None else d_status.data_ptr(), _raw_stream(_device()))
 
 
 def enec_dequantize_microscaled(d_in, in_size, dt, batch, rows, cols, d_out, ld, d_status=None) -> int:
     """The values of a microscaled stream in type dt, rows `ld` values apart."""
-    return lib().enec_dequantize_microscaled(_ptr(d_in), in_size, dt, batch, rows, cols, _ptr(d_out), ld, _ptr(d_status), _stream())
+    return _micro.enec_dequantize_microscaled(d_in.data_ptr(), in_size, dt, batch, rows, cols, None if d_out is None else d_out.data_ptr(), ld,
+                                              None if d_status is None else d_status.data_ptr(), _raw_stream(_device()))
 
 
 def enec_matmul_microscaled(d_x, dt, tokens, ld_x, d_w, w_size, rows, cols, d_y, ld_y, d_status=None) -> int:
     """d_y [tokens, rows] = d_x [tokens, cols] times the transpose of the microscaled stream d_w (one matrix of rows x cols)."""
-    return lib().enec_matmul_microscaled(_ptr(d_x), dt, tokens, ld_x, _ptr(d_w), w_size, rows, cols, _ptr(d_y), ld_y, _ptr(d_status), _stream())
+    return _micro.enec_matmul_microscaled(None if d_x is None else d_x.data_ptr(), dt, tokens, ld_x, d_w.data_ptr(), w_size, rows, cols,
+                                          d_y.data_ptr(), ld_y, None if d_status is None else d_status.data_ptr(), _raw_stream(_device()))
 
 
 def enec_matmul_microscaled_both(d_x, x_size, tokens, d_w, w_size, rows, cols, dt, d_y, ld_y, d_status=None) -> int:
     """The product of two microscaled streams, d_x (tokens x cols) and d_w (rows x cols), in type dt."""
-    return lib().enec_matmul_microscaled_both(_ptr(d_x), x_size, tokens, _ptr(d_w), w_size, rows, cols, dt, _ptr(d_y), ld_y, _ptr(d_status),
-                                              _stream())
+    return _micro.enec_matmul_microscaled_both(d_x.data_ptr(), x_size, tokens, d_w.data_ptr(), w_size, rows, cols, dt, d_y.data_ptr(), ld_y,
+                                               None if d_status is None else d_status.data_ptr(), _raw_stream(_device()))
 
 
 def enec_moe_microscaled_workspace(tokens: int, hidden: int, inter: int, experts: int, top_k: int) -> int:
-    return lib().enec_moe_microscaled_workspace(tokens, hidden, inter, experts, top_k)
+    return _micro.enec_moe_microscaled_workspace(tokens, hidden, inter, experts, top_k)
 
 
 def enec_moe_microscaled(d_x, dt, tokens, hidden, ld_x, d_router, experts, top_k, renormalize, d_gate, gate_size, d_up, up_size, d_down, down_size,
                          inter, d_y, ld_y, d_workspace, workspace_bytes, d_status=None) -> int:
     """A mixture-of-experts layer for few tokens; gate, up and down are microscaled streams of `experts` matrices."""
-    return lib().enec_moe_microscaled(_ptr(d_x), dt, tokens, hidden, ld_x, _ptr(d_router), experts, top_k, int(bool(renormalize)), _ptr(d_gate),
-                                      gate_size, _ptr(d_up), up_size, _ptr(d_down), down_size, inter, _ptr(d_y), ld_y, _ptr(d_workspace),
-                                      workspace_bytes, _ptr(d_status), _stream())
+    return _micro.enec_moe_microscaled(d_x.data_ptr(), dt, tokens, hidden, ld_x, d_router.data_ptr(), experts, top_k, 1 if renormalize else 0,
+                                       d_gate.data_ptr(), gate_size, d_up.data_ptr(), up_size, d_down.data_ptr(), down_size, inter, d_y.data_ptr(),
+                                       ld_y, d_workspace.data_ptr(), workspace_bytes, None if d_status is None else d_status.data_ptr(),
+                                       _raw_stream(_device()))
 
 
 def enec_launch_count() -> int:

@@ -3,10 +3,11 @@
 // Lanes of the accumulator are rows of W, its columns tokens: 128 x up to 192, twice, so that a tile's results leave while the next one's
 // products run. A CTA takes tile after tile. A stage is one record's 256 columns: a record lies in memory as the tensor cores want it in
 // shared memory, so a stage is a handful of bulk copies without a tensor map, and its scales go on to tensor memory as they are
-// (tcgen05.cp). At this rate a tile is bound by refilling shared memory: 44 KB a stage for 392 clocks of matrix instructions (98 each,
-// measured), of which L2 gave 84 bytes a clock at most. 256 x 192 needs 60 KB for twice the instructions, but only three such
-// stages fit, and no second set of sums: 2048 x 14336 x 4096 took 85 us, 1300 clocks a stage for want of copies on the way, and
-// storing 9000 clocks a tile behind the products.
+// (tcgen05.cp). At this rate a tile is bound by shared memory: a stage's 44 KB are written once, and its 4 matrix instructions read 10 KB
+// each, 85 KB in all or 664 clocks at 128 bytes a clock, for 392 clocks of instructions (98 each, measured); the kernel takes 840.
+// 256 x 192 would need 548 for the same work, but only three such stages fit, and no second set of sums: 2048 x 14336 x 4096 took
+// 85 us (1300 clocks a stage, and 9000 a tile for storing behind the products) against 68 us. Pairs of CTAs that share the tokens'
+// operand would read 57 KB.
 #include "enec_micro_mma.cuh"
 
 #include "enec_micro_launch.cuh"
@@ -204,14 +205,14 @@ extern "C" enec_status enec_matmul_microscaled_both(const void* d_x, size_t x_si
     job.y = static_cast<uint8_t*>(d_y);
     job.ld_y = ld_y;
     job.status = d_status;
-    // the tile whose rounds over the SMs cost least: a stage's time is that of its matrix instructions or of refilling shared memory at 84 bytes
-    // a clock, whichever is longer, and a CTA has some 5000 clocks of filling the ring and of storing its last tile. Tokens in steps of 64:
+    // the tile whose rounds over the SMs cost least: a stage's time is that of its matrix instructions or of shared memory's bytes, whichever is
+    // longer, and a CTA has some 5000 clocks of filling the ring and of storing its last tile. Tokens in steps of 64:
     // a tile then begins at row 0 or 64 of a record, and its scales at an even column of tensor memory.
     uint64_t least = ~uint64_t(0), tiles = 0;
     for (uint32_t k = kBothMostTokens; k >= 64; k -= 64) {
         const uint64_t all = uint64_t(job.sw.row_tiles) * ((tokens + k - 1) / k), rounds = (all + dev.sms - 1) / dev.sms;
-        const uint32_t instructions = 4 * (k > 128 ? k / 2 + 2 : 65), refill = (kMicroRecordBytes + k * 128 + 2048) / 84;
-        const uint64_t cost = rounds * job.sw.col_tiles * (instructions > refill ? instructions : refill) + 5000;
+        const uint32_t instructions = 4 * (k > 128 ? k / 2 + 2 : 65), bytes = 4 * (4096 + k * 32) + both_stage_bytes(k);
+        const uint64_t cost = rounds * job.sw.col_tiles * (instructions > bytes / 128 ? instructions : bytes / 128) + 5000;
         if (cost < least) least = cost, job.tile_tokens = k, tiles = all;
     }
     if (tiles >> 31) return ENEC_ERR_TOO_LARGE;

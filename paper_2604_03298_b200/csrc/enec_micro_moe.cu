@@ -163,42 +163,36 @@ __device__ __forceinline__ uint32_t logit_key(float v) {
 }
 
 // Parts of a CTA's columns that warps share in the router's products; and the bytes of its sums.
-__host__ __device__ inline uint32_t router_splits(uint32_t experts) {
-    const uint32_t tiles = (experts + 15) / 16;
+__host__ __device__ inline uint32_t router_splits(uint32_t tokens, uint32_t experts) {
+    const uint32_t tiles = (experts + 15) / 16 * ((tokens + 7) / 8);
     return tiles >= 16 ? 1 : 16 / tiles;
 }
-__host__ __device__ inline uint32_t router_bytes(uint32_t tokens, uint32_t experts) { return (1 + router_splits(experts)) * tokens * experts * 4; }
+__host__ __device__ inline uint32_t router_bytes(uint32_t tokens, uint32_t experts) {
+    return (1 + router_splits(tokens, experts)) * tokens * experts * 4;
+}
 
-// A warp: the `top` largest of `experts` logits of two tokens (two chains that do not wait for each other), ties to the lower number; lane
-// j gets the j-th. N: experts a lane looks after.
+// A warp: the `top` largest of `experts` logits, ties to the lower number; lane j gets the j-th. N: experts a lane looks after.
 template <uint32_t N>
-__device__ __forceinline__ uint2 choose_experts(const float* l0, const float* l1, uint32_t experts, uint32_t top, uint32_t lane) {
-    uint32_t keys[2][N];   // of experts lane, lane + 32, ..; 0 for those that do not exist or have been chosen
-    uint32_t mine[2] = {0, 0};
+__device__ __forceinline__ uint32_t choose_experts(const float* l, uint32_t experts, uint32_t top, uint32_t lane) {
+    uint32_t keys[N];   // of experts lane, lane + 32, ..; 0 for those that do not exist or have been chosen
 #pragma unroll
-    for (uint32_t i = 0; i < N; ++i) {
-        const bool there = lane + 32 * i < experts;
-        keys[0][i] = there ? logit_key(l0[lane + 32 * i]) : 0u;
-        keys[1][i] = there ? logit_key(l1[lane + 32 * i]) : 0u;
-    }
+    for (uint32_t i = 0; i < N; ++i) keys[i] = lane + 32 * i < experts ? logit_key(l[lane + 32 * i]) : 0u;
+    uint32_t mine = 0;
     for (uint32_t j = 0; j < top; ++j) {
+        uint32_t key = 0, at = 0;
 #pragma unroll
-        for (uint32_t k = 0; k < 2; ++k) {
-            uint32_t key = 0, at = 0;
-#pragma unroll
-            for (uint32_t i = 0; i < N; ++i) {
-                at = keys[k][i] > key ? i : at;
-                key = max(keys[k][i], key);
-            }
-            const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, key);
-            const uint32_t chosen = __reduce_min_sync(0xFFFFFFFFu, key == best ? lane + 32 * at : 0xFFFFFFFFu);
-            const uint32_t gone = (chosen & 31) == lane ? chosen >> 5 : N;
-#pragma unroll
-            for (uint32_t i = 0; i < N; ++i) keys[k][i] = i == gone ? 0u : keys[k][i];
-            mine[k] = lane == j ? chosen : mine[k];
+        for (uint32_t i = 0; i < N; ++i) {
+            at = keys[i] > key ? i : at;
+            key = max(keys[i], key);
         }
+        const uint32_t best = __reduce_max_sync(0xFFFFFFFFu, key);
+        const uint32_t chosen = __reduce_min_sync(0xFFFFFFFFu, key == best ? lane + 32 * at : 0xFFFFFFFFu);
+        const uint32_t gone = (chosen & 31) == lane ? chosen >> 5 : N;
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) keys[i] = i == gone ? 0u : keys[i];
+        mine = lane == j ? chosen : mine;
     }
-    return make_uint2(mine[0], mine[1]);
+    return mine;
 }
 
 // The router: logits of all tokens to every CTA of the cluster, then every warp chooses for its tokens.
@@ -209,56 +203,51 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
     const uint32_t total = job.tokens * job.experts;
     const uint32_t blocks = (job.hidden + 31) / 32, share = (blocks + kMoeCluster - 1) / kMoeCluster;
     const uint32_t b0 = min(rank * share, blocks), b1 = min(b0 + share, blocks);
-    // a warp takes 16 experts, all tokens and a part of the CTA's columns: the router's rows are read once, the tokens' once for each 16 experts
-    const uint32_t expert_tiles = (job.experts + 15) / 16, token_tiles = (job.tokens + 7) / 8;
-    const uint32_t splits = router_splits(job.experts), split_blocks = (share + splits - 1) / splits;
+    const uint32_t expert_tiles = (job.experts + 15) / 16, token_tiles = (job.tokens + 7) / 8, tiles = expert_tiles * token_tiles;
+    // where tiles are few, warps share a tile's columns too
+    const uint32_t splits = router_splits(job.tokens, job.experts), split_blocks = (share + splits - 1) / splits;
     float* logits = scratch;
     float* part = scratch + total;   // [split][token][expert]
     const bool whole = job.hidden % 32 == 0 && job.ld_x % 8 == 0;   // every load is of 16 aligned bytes
-    for (uint32_t unit = warp; unit < expert_tiles * splits; unit += kMoeWarps) {
-        const uint32_t tile = unit % expert_tiles, split = unit / expert_tiles;
-        const uint32_t e = tile * 16 + g;
+    for (uint32_t unit = warp; unit < tiles * splits; unit += kMoeWarps) {
+        const uint32_t tile = unit % tiles, split = unit / tiles;
+        const uint32_t e = tile % expert_tiles * 16 + g, token = tile / expert_tiles * 8 + g;
         // rows that do not exist are read from the last one's place and not written
         const uint8_t* r0 = job.router + uint64_t(min(e, job.experts - 1)) * job.hidden * 2;
         const uint8_t* r1 = job.router + uint64_t(min(e + 8, job.experts - 1)) * job.hidden * 2;
+        const uint8_t* xr = job.x + uint64_t(min(token, job.tokens - 1)) * job.ld_x * 2;
         const uint32_t first = min(b0 + split * split_blocks, b1), last = min(first + split_blocks, b1);
-        constexpr uint32_t kTiles = kMoeMostTokens / 8;
-        float c[kTiles][4] = {};
-#pragma unroll 2
-        for (uint32_t b = first; b < last; ++b) {
-            const uint32_t col = 32 * b + 8 * t;
-            uint32_t a0[4], a1[4], bx[kTiles][4];
-            if (whole) {
-                const uint4 v0 = __ldg(reinterpret_cast<const uint4*>(r0 + col * 2)), v1 = __ldg(reinterpret_cast<const uint4*>(r1 + col * 2));
-                a0[0] = v0.x, a0[1] = v0.y, a0[2] = v0.z, a0[3] = v0.w;
-                a1[0] = v1.x, a1[1] = v1.y, a1[2] = v1.z, a1[3] = v1.w;
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
+        constexpr uint32_t kBatch = 4;
+        for (uint32_t b = first; b < last; b += kBatch) {
+            uint32_t a0[kBatch][4], a1[kBatch][4], bx[kBatch][4];
+            if (whole && b + kBatch <= last) {
 #pragma unroll
-                for (uint32_t i = 0; i < kTiles; ++i) {
-                    if (i >= token_tiles) break;
-                    const uint4 v = __ldg(reinterpret_cast<const uint4*>(job.x + (uint64_t(min(8 * i + g, job.tokens - 1)) * job.ld_x + col) * 2));
-                    bx[i][0] = v.x, bx[i][1] = v.y, bx[i][2] = v.z, bx[i][3] = v.w;
+                for (uint32_t i = 0; i < kBatch; ++i) {
+                    const uint64_t at = uint64_t(32 * (b + i) + 8 * t) * 2;
+                    const uint4 v0 = __ldg(reinterpret_cast<const uint4*>(r0 + at)), v1 = __ldg(reinterpret_cast<const uint4*>(r1 + at)),
+                                v2 = __ldg(reinterpret_cast<const uint4*>(xr + at));
+                    a0[i][0] = v0.x, a0[i][1] = v0.y, a0[i][2] = v0.z, a0[i][3] = v0.w;
+                    a1[i][0] = v1.x, a1[i][1] = v1.y, a1[i][2] = v1.z, a1[i][3] = v1.w;
+                    bx[i][0] = v2.x, bx[i][1] = v2.y, bx[i][2] = v2.z, bx[i][3] = v2.w;
                 }
             } else {
-                const int valid = col < job.hidden ? int(min(job.hidden - col, 8u)) : 0;
-                load_eight<DT>(r0 + col * 2, valid, a0);
-                load_eight<DT>(r1 + col * 2, valid, a1);
 #pragma unroll
-                for (uint32_t i = 0; i < kTiles; ++i) {
-                    if (i >= token_tiles) break;
-                    load_eight<DT>(job.x + (uint64_t(min(8 * i + g, job.tokens - 1)) * job.ld_x + col) * 2, valid, bx[i]);
+                for (uint32_t i = 0; i < kBatch; ++i) {
+                    const uint32_t col = 32 * (b + i) + 8 * t;
+                    const int valid = b + i < last && col < job.hidden ? int(min(job.hidden - col, 8u)) : 0;
+                    load_eight<DT>(r0 + uint64_t(col) * 2, valid, a0[i]);
+                    load_eight<DT>(r1 + uint64_t(col) * 2, valid, a1[i]);
+                    load_eight<DT>(xr + uint64_t(col) * 2, valid, bx[i]);
                 }
             }
 #pragma unroll
-            for (uint32_t i = 0; i < kTiles; ++i)
-                if (i < token_tiles) mma_native<DT>(c[i], a0, a1, bx[i]);
+            for (uint32_t i = 0; i < kBatch; ++i) mma_native<DT>(c, a0[i], a1[i], bx[i]);
         }
 #pragma unroll
-        for (uint32_t tt = 0; tt < kTiles; ++tt) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t ee = tile * 16 + g + (i >> 1) * 8, token = tt * 8 + 2 * t + (i & 1);
-                if (ee < job.experts && token < job.tokens) part[split * total + token * job.experts + ee] = c[tt][i];
-            }
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t ee = tile % expert_tiles * 16 + g + (i >> 1) * 8, tt = tile / expert_tiles * 8 + 2 * t + (i & 1);
+            if (ee < job.experts && tt < job.tokens) part[split * total + tt * job.experts + ee] = c[i];
         }
     }
     if (splits > 1) {
@@ -279,29 +268,23 @@ __device__ __forceinline__ void route(const MoeJob& job, const Routing& r, float
         for (uint32_t k = 0; k < kMoeCluster; ++k) cluster.map_shared_rank(logits, k)[i] = v;
     }
     cluster.sync();
-    for (uint32_t first = warp; first < job.tokens; first += 2 * kMoeWarps) {
-        const uint32_t second = min(first + kMoeWarps, job.tokens - 1);
-        const float *l0 = logits + first * job.experts, *l1 = logits + second * job.experts;
-        const uint2 chosen = job.experts <= 64    ? choose_experts<2>(l0, l1, job.experts, job.top, lane)
-                             : job.experts <= 128 ? choose_experts<4>(l0, l1, job.experts, job.top, lane)
-                                                  : choose_experts<kMoeMostExperts / 32>(l0, l1, job.experts, job.top, lane);
+    for (uint32_t token = warp; token < job.tokens; token += kMoeWarps) {
+        const float* l = logits + token * job.experts;
+        const uint32_t my_expert = job.experts <= 64    ? choose_experts<2>(l, job.experts, job.top, lane)
+                                   : job.experts <= 128 ? choose_experts<4>(l, job.experts, job.top, lane)
+                                                        : choose_experts<kMoeMostExperts / 32>(l, job.experts, job.top, lane);
+        float my_logit = 0.f;
+        if (lane < job.top) my_logit = l[my_expert];
+        const float highest = __shfl_sync(0xFFFFFFFFu, my_logit, 0);
+        const float mine = lane < job.top ? expf(my_logit - highest) : 0.f;
+        float sum = job.renormalize ? mine : 0.f;
+        if (!job.renormalize)
+            for (uint32_t e = lane; e < job.experts; e += 32) sum += expf(l[e] - highest);
 #pragma unroll
-        for (uint32_t k = 0; k < 2; ++k) {
-            if (k == 1 && first + kMoeWarps >= job.tokens) break;
-            const float* l = k ? l1 : l0;
-            const uint32_t token = k ? second : first, mine_expert = k ? chosen.y : chosen.x;
-            const float my_logit = lane < job.top ? l[mine_expert] : 0.f;
-            const float highest = __shfl_sync(0xFFFFFFFFu, my_logit, 0);
-            const float mine = lane < job.top ? expf(my_logit - highest) : 0.f;
-            float sum = job.renormalize ? mine : 0.f;
-            if (!job.renormalize)
-                for (uint32_t e = lane; e < job.experts; e += 32) sum += expf(l[e] - highest);
-#pragma unroll
-            for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-            if (lane < job.top) {
-                r.weight[token * job.top + lane] = mine / sum;
-                r.expert[token * job.top + lane] = uint16_t(mine_expert);
-            }
+        for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+        if (lane < job.top) {
+            r.weight[token * job.top + lane] = mine / sum;
+            r.expert[token * job.top + lane] = uint16_t(my_expert);
         }
     }
     __syncthreads();
