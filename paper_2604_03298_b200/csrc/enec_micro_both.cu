@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
     const uint32_t n = job.tile_tokens, stage_bytes = both_stage_bytes(n);
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < job.stages; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
-        for (uint32_t i = 0; i < 2; ++i) mbar_init(done + i, 1), mbar_init(drained + i, kBothThreads - 64);
+        for (uint32_t i = 0; i < 2; ++i) mbar_init(done + i, 1), mbar_init(drained + i, kBothThreads / 32 - 2);
         mbar_fence_init();
         failed = 0;
     }
@@ -104,20 +104,23 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
     } else if (warp == 1) {
         const uint32_t idesc = scaled_idesc(n);
         const uint64_t operands = operand_desc(smem_u32(smem)), scales = scale_desc(smem_u32(smem) + kMicroElemBytes + n * 128);
-        uint32_t s = 0, phase = 0, i = 0;
+        uint32_t s = 0, phase = 0, i = 0, there = mbar_complete(full, 0);
         for (uint32_t t = blockIdx.x; t < job.tiles; t += gridDim.x, ++i) {
             const BothTile tile(job, t);
             const uint32_t set = i & 1, sums = tmem + set * kBothMostTokens;
             if (i >= 2 && !suspended_wait(drained + set, ((i >> 1) - 1) & 1, &failed)) failed = 1;
             for (uint32_t k = 0; k < records && !failed; ++k) {
-                if (!suspended_wait(full + s, phase, &failed)) {
+                if (!there && !suspended_wait(full + s, phase, &failed)) {
                     failed = 1;
                     break;
                 }
+                const uint32_t now = s;
+                if (++s == job.stages) s = 0, phase ^= 1;
+                there = mbar_complete(full + s, phase);
                 tcgen05_fence_after();
-                const uint64_t a = operands + s * (stage_bytes / 16), b = a + kMicroElemBytes / 16, sc = scales + s * (stage_bytes / 16);
+                const uint64_t a = operands + now * (stage_bytes / 16), b = a + kMicroElemBytes / 16, sc = scales + now * (stage_bytes / 16);
                 // tensor memory of a stage's scales: of the columns' four chunks h, 4 columns for the rows of W, and 8 for the tokens
-                const uint32_t to = tmem + 2 * kBothMostTokens + s * kScaleColumns;
+                const uint32_t to = tmem + 2 * kBothMostTokens + now * kScaleColumns;
 #pragma unroll
                 for (uint32_t h = 0; h < 2; ++h) {
                     copy_scales(leader, to + h * 4, sc + h * 32);
@@ -131,8 +134,7 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
                     mma_scaled(q < steps ? leader : 0, sums, a + q * 2, b + q * 2, idesc | pair << 4 | pair << 29, to + h * 4,
                                to + 8 + h * 8 + tile.skip / 32, k > 0 || q > 0);
                 }
-                tcgen05_commit(leader, empty + s);
-                if (++s == job.stages) s = 0, phase ^= 1;
+                tcgen05_commit(leader, empty + now);
             }
             tcgen05_commit(leader, done + set);
         }
@@ -158,7 +160,7 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
                 }
             }
             tcgen05_fence_before();
-            mbar_arrive(drained + set);
+            warp_arrive(drained + set);
         }
         if (!good && blockIdx.x == 0 && warp == 2 && lane == 0) report(job.status, ENEC_ERR_BAD_STREAM);
     }

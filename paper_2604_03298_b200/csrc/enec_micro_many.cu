@@ -27,7 +27,8 @@ namespace {
 constexpr uint32_t kFirstX = 2, kFirstW = 10, kThreadsX = 8 * 32;
 template <int MT>
 __host__ __device__ constexpr uint32_t many_threads() { return (kFirstW + 8 * MT) * 32; }
-constexpr uint32_t kStagesA = 5, kStagesB = 3;   // of 128 rows x 64 columns of weights; of the tokens x 64 columns of x
+// Stages of 128 rows x 64 columns of weights; of the tokens x 64 columns of x, at least and at most; of raw records, at most, as many as fit.
+constexpr uint32_t kStagesA = 5, kLeastB = 3, kMostB = 10, kMostRaw = 4;
 constexpr uint32_t kManyMostTokens = 256;
 
 struct ManyJob {
@@ -42,18 +43,15 @@ struct ManyJob {
     uint32_t row_tiles;      // tiles along the rows
     uint32_t cluster;        // CTAs that share a tile's columns
     uint32_t share;          // records of columns each takes
+    uint32_t stages_b, stages_raw;
     uint32_t aligned;        // rows of x begin on 16-byte boundaries: tiles of it come by the tensor map
     CUtensorMap map;
     int* status;
 };
 
-// Records of raw weights on the way or in use: one where shared memory is short, two where it is not and latency counts.
 template <int MT>
-__host__ __device__ constexpr uint32_t raw_stages() { return MT == 1 ? 2 : 1; }
-
-template <int MT>
-__host__ __device__ constexpr uint32_t many_bytes(uint32_t tokens) {
-    return raw_stages<MT>() * MT * kMicroRecordBytes + kStagesA * 16384 + kStagesB * tokens * 128 + 1024;
+__host__ __device__ constexpr uint32_t many_bytes(uint32_t tokens, uint32_t stages_b, uint32_t stages_raw) {
+    return stages_raw * MT * kMicroRecordBytes + kStagesA * 16384 + stages_b * tokens * 128 + 1024;
 }
 
 // 64 columns x tile_tokens rows of x from (column, token) on; zeros behind the matrix.
@@ -99,8 +97,7 @@ __device__ __forceinline__ uint4 to_values(uint32_t codes, uint32_t factor) {
 template <int DT, int MT>
 __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(const __grid_constant__ ManyJob job) {
     extern __shared__ uint8_t raw_shared[];
-    constexpr uint32_t kRaw = raw_stages<MT>();
-    __shared__ uint64_t raw_full[raw_stages<MT>()], raw_empty[raw_stages<MT>()], full_a[kStagesA], empty_a[kStagesA], full_b[kStagesB], empty_b[kStagesB], done;
+    __shared__ uint64_t raw_full[kMostRaw], raw_empty[kMostRaw], full_a[kStagesA], empty_a[kStagesA], full_b[kMostB], empty_b[kMostB], done;
     __shared__ uint32_t tmem_at;
     __shared__ volatile int failed;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -109,9 +106,9 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
     uint32_t tmem_columns = 32;
     while (tmem_columns < MT * n) tmem_columns *= 2;
     if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < kRaw; ++i) mbar_init(raw_full + i, 1), mbar_init(raw_empty + i, 256 * MT);
-        for (uint32_t i = 0; i < kStagesA; ++i) mbar_init(full_a + i, 256), mbar_init(empty_a + i, 1);
-        for (uint32_t i = 0; i < kStagesB; ++i) mbar_init(full_b + i, job.aligned ? 1 : kThreadsX), mbar_init(empty_b + i, 1);
+        for (uint32_t i = 0; i < job.stages_raw; ++i) mbar_init(raw_full + i, 1), mbar_init(raw_empty + i, 8 * MT);
+        for (uint32_t i = 0; i < kStagesA; ++i) mbar_init(full_a + i, 8), mbar_init(empty_a + i, 1);
+        for (uint32_t i = 0; i < job.stages_b; ++i) mbar_init(full_b + i, job.aligned ? 1 : kThreadsX / 32), mbar_init(empty_b + i, 1);
         mbar_init(&done, 1);
         mbar_fence_init();
         failed = 0;
@@ -135,15 +132,14 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
     const uint8_t* wr = job.w + kMicroHeaderBytes + row_tile * strip + uint64_t(k0) * kMicroRecordBytes;
     uint8_t* a_ring = smem;
     uint8_t* b_ring = a_ring + kStagesA * 16384;
-    uint8_t* raw = b_ring + kStagesB * n * 128;
+    uint8_t* raw = b_ring + job.stages_b * n * 128;
     const bool good = micro_header_ok(job.w, job.s);
 
     const uint32_t leader = elected();
     if (warp == 0) {
-        uint32_t k = 0;
+        uint32_t k = 0, s = 0, phase = 1;
         for (; k < records; ++k) {
-            const uint32_t s = k % kRaw;
-            if (k >= kRaw && !suspended_wait(raw_empty + s, (k / kRaw - 1) & 1, &failed)) {
+            if (k >= job.stages_raw && !suspended_wait(raw_empty + s, phase, &failed)) {
                 failed = 1;
                 break;
             }
@@ -152,46 +148,50 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
                 for (uint32_t i = 0; i < mt; ++i)
                     bulk_g2s(raw + (s * MT + i) * kMicroRecordBytes, wr + i * strip + uint64_t(k) * kMicroRecordBytes, kMicroRecordBytes, raw_full + s);
             }
+            if (++s == job.stages_raw) s = 0, phase ^= 1;
         }
         // nothing may be in flight when the CTA ends
-        for (uint32_t i = k > kRaw ? k - kRaw : 0; i < k; ++i) mbar_wait_bounded(raw_full + i % kRaw, (i / kRaw) & 1);
+        for (uint32_t i = k > job.stages_raw ? k - job.stages_raw : 0; i < k; ++i)
+            mbar_wait_bounded(raw_full + i % job.stages_raw, (i / job.stages_raw) & 1);
     } else if (warp == 1) {
         const uint32_t idesc = idesc_16bit(DT == ENEC_BF16, n);
         const uint64_t a0 = operand_desc(smem_u32(a_ring)), b0 = operand_desc(smem_u32(b_ring));
-        uint32_t slot = 0, phase = 0;
-        for (uint32_t j = 0; j < steps; ++j) {
-            const uint32_t sb = j % kStagesB;
-            bool there = suspended_wait(full_b + sb, (j / kStagesB) & 1, &failed);
+        uint32_t slot = 0, phase = 0, sb = 0, phase_b = 0;
+        uint32_t a_there = mbar_complete(full_a, 0), b_there = mbar_complete(full_b, 0);
+        bool there = true;
+        for (uint32_t j = 0; j < steps && there; ++j) {
+            const uint32_t sb_now = sb;
             const uint64_t b = b0 + sb * n * 8;
+            there = b_there || suspended_wait(full_b + sb, phase_b, &failed);
+            if (++sb == job.stages_b) sb = 0, phase_b ^= 1;
+            b_there = mbar_complete(full_b + sb, phase_b);
             for (uint32_t i = 0; i < mt && there; ++i) {
-                there = suspended_wait(full_a + slot, phase, &failed);
+                const uint32_t now = slot;
+                const uint64_t a = a0 + slot * 1024;
+                there = a_there || suspended_wait(full_a + slot, phase, &failed);
+                if (++slot == kStagesA) slot = 0, phase ^= 1;
+                a_there = mbar_complete(full_a + slot, phase);
                 if (!there) break;
                 tcgen05_fence_after();
-                const uint64_t a = a0 + slot * 1024;
 #pragma unroll
                 for (uint32_t q = 0; q < 4; ++q) mma_16bit(leader, tmem + i * n, a + q * 2, b + q * 2, idesc, j > 0 || q > 0);
-                tcgen05_commit(leader, empty_a + slot);
-                if (++slot == kStagesA) slot = 0, phase ^= 1;
+                tcgen05_commit(leader, empty_a + now);
             }
-            if (!there) {
-                failed = 1;
-                break;
-            }
-            tcgen05_commit(leader, empty_b + sb);
+            if (there) tcgen05_commit(leader, empty_b + sb_now);
         }
+        if (!there) failed = 1;
         tcgen05_commit(leader, &done);
         mbar_wait_bounded(&done, 0);   // no instruction may be under way when tensor memory is given back
     } else if (warp < kFirstW) {
         // x: eight lanes a row of 64 columns
         const uint32_t me = threadIdx.x - kFirstX * 32, c = me & 7;
-        uint32_t asked = 0;
+        uint32_t asked = 0, sb = 0, phase = 1;
         const uint32_t first_col = min(k0 * kMicroCols, job.s.cols);
         const uint8_t* from = job.x + (uint64_t(token0) * job.ld_x + first_col) * 2;
         bool ok = true;
         if (job.aligned) {
             for (uint32_t j = 0; j < steps && warp == kFirstX; ++j) {
-                const uint32_t sb = j % kStagesB;
-                if (j >= kStagesB && !suspended_wait(empty_b + sb, (j / kStagesB - 1) & 1, &failed)) {
+                if (j >= job.stages_b && !suspended_wait(empty_b + sb, phase, &failed)) {
                     ok = false;
                     break;
                 }
@@ -200,9 +200,11 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
                     tile_g2s(smem_u32(b_ring) + sb * n * 128, &job.map, first_col + j * 64, token0, full_b + sb);
                 }
                 asked = j + 1;
+                if (++sb == job.stages_b) sb = 0, phase ^= 1;
             }
             // nothing may be in flight when the CTA ends
-            for (uint32_t j = asked > kStagesB ? asked - kStagesB : 0; j < asked; ++j) mbar_wait_bounded(full_b + j % kStagesB, (j / kStagesB) & 1);
+            for (uint32_t j = asked > job.stages_b ? asked - job.stages_b : 0; j < asked; ++j)
+                mbar_wait_bounded(full_b + j % job.stages_b, (j / job.stages_b) & 1);
         } else {
             // rows that lie anywhere: through registers, 64 rows of a step at a time, the loads of three such batches on the way together
             constexpr uint32_t kAhead = 3;
@@ -222,9 +224,9 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
             for (uint32_t batch0 = 0; batch0 < all && ok; batch0 += kAhead) {
 #pragma unroll
                 for (uint32_t a = 0; a < kAhead; ++a) {
-                    const uint32_t batch = batch0 + a, j = batch / batches, part = batch - j * batches, sb = j % kStagesB;
+                    const uint32_t batch = batch0 + a, j = batch / batches, part = batch - j * batches;
                     if (batch >= all || !ok) break;
-                    if (part == 0 && j >= kStagesB && !suspended_wait(empty_b + sb, (j / kStagesB - 1) & 1, &failed)) {
+                    if (part == 0 && j >= job.stages_b && !suspended_wait(empty_b + sb, phase, &failed)) {
                         ok = false;
                         break;
                     }
@@ -238,7 +240,8 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
                     load(v[a], batch + kAhead);
                     if (part == batches - 1) {
                         fence_async_shared();
-                        mbar_arrive(full_b + sb);
+                        warp_arrive(full_b + sb);
+                        if (++sb == job.stages_b) sb = 0, phase ^= 1;
                     }
                 }
             }
@@ -266,21 +269,23 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e) place[e] = ((4 * half + e) ^ (r & 7)) << 4;
         bool ok = true;
+        uint32_t s = 0, phase = 0;
         for (uint32_t k = 0; k < records && ok; ++k) {
-            if (!suspended_wait(raw_full + k % kRaw, (k / kRaw) & 1, &failed)) {
+            if (!suspended_wait(raw_full + s, phase, &failed)) {
                 ok = false;
                 break;
             }
             uint4 codes[4];
             uint2 scales = {};   // eight bytes
-            const uint32_t rec = smem_u32(raw) + (k % kRaw * MT + i) * kMicroRecordBytes;
+            const uint32_t rec = smem_u32(raw) + (s * MT + i) * kMicroRecordBytes;
             if (mine) {
 #pragma unroll
                 for (uint32_t q = 0; q < 4; ++q) codes[q] = lds128(rec + r * 128 + (((2 * q + half) ^ (r & 7)) << 4));
                 const uint32_t at = rec + kMicroElemBytes + (r & 31) * 16 + (r >> 5) * 4;
                 scales = make_uint2(lds32(at), lds32(at + 512));
             }
-            mbar_arrive(raw_empty + k % kRaw);
+            warp_arrive(raw_empty + s);
+            if (++s == job.stages_raw) s = 0, phase ^= 1;
             const uint32_t here = min(4u, steps - 4 * k);
 #pragma unroll
             for (uint32_t q = 0; q < 4; ++q) {
@@ -307,7 +312,7 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
                         for (uint32_t e = 0; e < 4; ++e) sts128(dst + place[e], to_values<DT>(w[e], factor));
                     }
                     fence_async_shared();
-                    mbar_arrive(full_a + sa);
+                    warp_arrive(full_a + sa);
                 }
             }
         }
@@ -375,13 +380,17 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
 }
 
 template <int DT, int MT>
-enec_status launch_many(const ManyJob& job, uint32_t tiles, const MicroDevice& dev, cudaStream_t stream) {
+enec_status launch_many(ManyJob job, uint32_t tiles, const MicroDevice& dev, cudaStream_t stream) {
     static std::atomic<uint64_t> allowed{0};
-    if (!allow_shared(allowed, dev, enec_micro_many_kernel<DT, MT>, many_bytes<MT>(kManyMostTokens))) return ENEC_ERR_CUDA;
+    if (!allow_shared(allowed, dev, enec_micro_many_kernel<DT, MT>, kFewMostShared)) return ENEC_ERR_CUDA;
+    // raw records first, then x, as far as there is room
+    job.stages_b = kLeastB, job.stages_raw = 1;
+    while (job.stages_raw < kMostRaw && many_bytes<MT>(job.tile_tokens, job.stages_b, job.stages_raw + 1) <= kFewMostShared) ++job.stages_raw;
+    while (job.stages_b < kMostB && many_bytes<MT>(job.tile_tokens, job.stages_b + 1, job.stages_raw) <= kFewMostShared) ++job.stages_b;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(tiles * job.cluster);
     cfg.blockDim = dim3(many_threads<MT>());
-    cfg.dynamicSmemBytes = many_bytes<MT>(job.tile_tokens);
+    cfg.dynamicSmemBytes = many_bytes<MT>(job.tile_tokens, job.stages_b, job.stages_raw);
     if (job.cluster > 1 && cfg.dynamicSmemBytes < job.tile_tokens * kMicroRows * 4 + 1024) cfg.dynamicSmemBytes = job.tile_tokens * kMicroRows * 4 + 1024;
     const uint32_t least = MT * job.tile_tokens > 256 ? kTmemAloneShared : kTmemHalfShared;
     if (cfg.dynamicSmemBytes < least) cfg.dynamicSmemBytes = least;

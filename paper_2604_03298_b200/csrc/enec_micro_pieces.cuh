@@ -54,8 +54,8 @@ struct PieceTask {
 __device__ __forceinline__ void piece_setup(PieceShared& sh, uint32_t stages) {
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < stages; ++i) mbar_init(sh.full + i, 1), mbar_init(sh.empty + i, 1);
-        for (uint32_t i = 0; i < kPieceBatches; ++i) mbar_init(sh.staged + i, kPieceWorkers * 32);
-        for (uint32_t i = 0; i < 2; ++i) mbar_init(sh.done + i, 1), mbar_init(sh.drained + i, kPieceWorkers * 32);
+        for (uint32_t i = 0; i < kPieceBatches; ++i) mbar_init(sh.staged + i, kPieceWorkers);
+        for (uint32_t i = 0; i < 2; ++i) mbar_init(sh.done + i, 1), mbar_init(sh.drained + i, kPieceWorkers);
         mbar_fence_init();
         sh.failed = 0;
     }
@@ -162,7 +162,7 @@ __device__ __forceinline__ void stage_digits(PieceShared& sh, uint32_t worker, u
                 if (first + j * kPieceWorkers < sweeps.total) put_digits(x[j], column[j], at + record[j] * record_bytes, columns, lane);
         }
         fence_async_shared();
-        mbar_arrive(sh.staged + batch);
+        warp_arrive(sh.staged + batch);
     }
 }
 
@@ -215,6 +215,7 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
         const uint64_t ring_desc = operand_desc(ring), ring_scales_desc = scale_desc(ring + kMicroElemBytes);
         const uint64_t digits_desc = operand_desc(digits), digit_scales_desc = scale_desc(digits);
         uint32_t group = 0xFFFFFFFFu, slot = 0, phase = 0;
+        uint32_t full_there = mbar_complete(sh.full, 0);
         uint32_t flipped = 0;   // bit b: announcements of batch b so far, mod 2
         volatile int never = 0;
         for (uint32_t i = 0; i < n_tasks; ++i, tasks.next()) {
@@ -230,7 +231,10 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
             const uint32_t idesc = scaled_idesc(columns), record16 = columns * 8 + 64;   // a record's digits in units of 16 bytes
             uint64_t b = digits_desc, bs = digit_scales_desc + columns * 8;
             for (uint32_t k = 0; k < task.count && !sh.failed; ++k) {
-                bool there = suspended_wait(sh.full + slot, phase, &sh.failed);
+                const uint32_t now = slot;
+                bool there = full_there || suspended_wait(sh.full + slot, phase, &sh.failed);
+                if (++slot == stages) slot = 0, phase ^= 1;
+                full_there = mbar_complete(sh.full + slot, phase);
                 if (known < sweeps.batches) {
                     const uint32_t batch = sweeps.batch_of(k, task.n);
                     for (; there && known <= batch; ++known) there = suspended_wait(sh.staged + known, flipped >> known & 1, &sh.failed);
@@ -240,8 +244,8 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
                     break;
                 }
                 tcgen05_fence_after();
-                const uint64_t a = ring_desc + slot * (kMicroRecordBytes / 16), as = ring_scales_desc + slot * (kMicroRecordBytes / 16);
-                const uint32_t to = tmem + 2 * kPieceTokens * kPieces + slot * 16;
+                const uint64_t a = ring_desc + now * (kMicroRecordBytes / 16), as = ring_scales_desc + now * (kMicroRecordBytes / 16);
+                const uint32_t to = tmem + 2 * kPieceTokens * kPieces + now * 16;
                 copy_scales(leader, to, as);
                 copy_scales(leader, to + 8, bs);
                 copy_scales(leader, to + 4, as + 32);
@@ -253,9 +257,8 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
                     mma_scaled(q < steps ? leader : 0, sums, a + q * 2, b + q * 2, idesc | pair << 4 | pair << 29, to + h * 4, to + 8 + h * 4,
                                k > 0 || q > 0);
                 }
-                tcgen05_commit(leader, sh.empty + slot);
+                tcgen05_commit(leader, sh.empty + now);
                 b += record16, bs += record16;
-                if (++slot == stages) slot = 0, phase ^= 1;
             }
             if (begins) flipped ^= (1u << sweeps.batches) - 1;
             tcgen05_commit(leader, sh.done + set);
@@ -277,7 +280,7 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
             const bool ok = !sh.failed;
             take(i, tmem + set * (kPieceTokens * kPieces) + ((warp & 3) * 32 << 16), ok);
             tcgen05_fence_before();
-            mbar_arrive(sh.drained + set);
+            warp_arrive(sh.drained + set);
             after(i, ok);
             if (lockstep) meet(i);
         }
