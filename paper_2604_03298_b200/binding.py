@@ -344,8 +344,9 @@ def quantize_tensor(t: torch.Tensor) -> torch.Tensor:
     size = enec_microscaled_size(batch, rows, cols)
     if size == 0:
         raise EnecError(-8, "enec_microscaled_size")
-    out = torch.empty(size, dtype=torch.uint8, device=t.device)
-    st = enec_quantize_microscaled(t, dt, batch, rows, cols, ld, out, size)
+    with torch.cuda.device(t.device):
+        out = torch.empty(size, dtype=torch.uint8, device=t.device)
+        st = enec_quantize_microscaled(t, dt, batch, rows, cols, ld, out, size)
     if st != 0:
         raise EnecError(st, "enec_quantize_microscaled")
     return out
@@ -355,9 +356,10 @@ def dequantize_tensor(stream: torch.Tensor, dtype: torch.dtype, shape) -> torch.
     """The values of a stream of quantize_tensor in `dtype`; waits for the current stream once to learn whether the header fits."""
     shape = tuple(shape)
     batch, rows, cols = shape if len(shape) == 3 else (1, *shape)
-    out = torch.empty(shape, dtype=dtype, device=stream.device)
-    a, stream_handle = _answer()
-    st = lib().enec_dequantize_microscaled(stream.data_ptr(), stream.numel(), _DT[dtype], batch, rows, cols, out.data_ptr(), cols, a.status_at,
-                                           stream_handle)
-    _finish(a, st, "enec_dequantize_microscaled")
+    with torch.cuda.device(stream.device):
+        out = torch.empty(shape, dtype=dtype, device=stream.device)
+        a, stream_handle = _answer()
+        st = lib().enec_dequantize_microscaled(stream.data_ptr(), stream.numel(), _DT[dtype], batch, rows, cols, out.data_ptr(), cols, a.status_at,
+                                               stream_handle)
+        _finish(a, st, "enec_dequantize_microscaled")
     return out

@@ -18,7 +18,6 @@ struct MicroProduct {
 };
 
 constexpr uint32_t kFewMostShared = 226 * 1024;   // the kernels have a little static shared memory beside it
-constexpr uint32_t kFewHalfShared = 228 * 1024 / 2 - 1024;   // two CTAs on an SM: each has a kilobyte of the system's beside its own
 
 // Whether the form for few tokens takes a call (up to 16 tokens, as long as their digits fit into a cluster's shared memory).
 bool micro_few_takes(uint32_t tokens, uint32_t col_tiles);

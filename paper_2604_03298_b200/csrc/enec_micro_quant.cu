@@ -92,8 +92,14 @@ __global__ void __launch_bounds__(kQuantThreads) enec_micro_quantize_kernel(cons
         float x[8];
         as_floats<DT>(w[q], x);
         uint32_t top = 0;   // the order of magnitudes is the order of their bits; a NaN's are the largest
+        if constexpr (DT == ENEC_FP32) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+            for (int i = 0; i < 8; ++i) top = max(top, w[q][i] & 0x7FFFFFFFu);
+        } else {   // two at a time, in their own type
+            uint32_t two = __vmaxu2(__vmaxu2(w[q][0] & 0x7FFF7FFFu, w[q][1] & 0x7FFF7FFFu), __vmaxu2(w[q][2] & 0x7FFF7FFFu, w[q][3] & 0x7FFF7FFFu));
+            two = max(two >> 16, two & 0xFFFFu);
+            top = DT == ENEC_BF16 ? two << 16 : __float_as_uint(MicroType<ENEC_FP16>::unpack(two).x);
+        }
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
         const uint32_t exponent = top >> 23;   // floor(log2) + 127, and 0 for zero and subnormal numbers

@@ -251,3 +251,45 @@ def test_repeated_captured_and_concurrent_calls_agree_bit_for_bit(tokens):
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(ys[0], y) for y in ys[1:])
+
+
+def test_quantize_tensor_takes_views():
+    """Rows apart, transposed, unaligned and broadcast views: the stream is that of the dense copy."""
+    E = enec()
+    wide = torch.randn(70, 400, device="cuda").to(torch.float16)
+    for view in (wide[:, :300], wide[3:, 8:], wide[:, 1:], wide.t(), wide[:1].expand(5, 400), wide[::2]):
+        got = E.quantize_tensor(view)
+        assert torch.equal(got, E.quantize_tensor(view.contiguous().clone()))
+        assert np.array_equal(got.cpu().numpy(), ref.stream(view.cpu().double().numpy()[None]))
+    with pytest.raises(ValueError):
+        E.quantize_tensor(wide[0])
+
+
+def test_layer_of_products_one_after_another():
+    """As they are used together: a decoder layer's gate, up and down products of a few tokens on streams made from one checkpoint tensor,
+    the same layer for a prompt, and the same with 4-bit activations; the three agree where they compute the same."""
+    E = enec()
+    hidden, ffn = 512, 1100
+    g = torch.Generator().manual_seed(3)
+    ws = [E.quantize_tensor((torch.randn(r, c, generator=g) * c ** -0.5).to(torch.bfloat16).cuda()) for r, c in ((ffn, hidden), (ffn, hidden), (hidden, ffn))]
+    x = torch.randn(300, hidden, generator=g).to(torch.bfloat16).cuda()
+
+    def product(x, w, rows):
+        y = torch.empty(x.shape[0], rows, dtype=x.dtype, device="cuda")
+        assert E.enec_matmul_microscaled(x, 0, x.shape[0], x.shape[1], w, w.numel(), rows, x.shape[1], y, rows) == 0
+        return y
+
+    def layer(x):
+        a, u = product(x, ws[0], ffn), product(x, ws[1], ffn)
+        return product((torch.nn.functional.silu(a.float()) * u.float()).to(x.dtype), ws[2], hidden)
+    many, few = layer(x), torch.cat([layer(x[i:i + 10].contiguous()) for i in range(0, 300, 10)])
+    # Both forms round their results once. Where an exact sum lies beside a border between two bf16 values they may fall on either side, one
+    # step (at most 2^-7 of the value) apart: a and u, through |silu'| <= 1.1, then their rounded product, then y. 1.05 covers the steps'
+    # own products and the fp32 sums, which are 2^-11 of the steps.
+    v = [torch.from_numpy(ref.values(E.dequantize_tensor(w, torch.float32, s).cpu().numpy())) for w, s in zip(ws, ((ffn, hidden), (ffn, hidden), (hidden, ffn)))]
+    a, u = x.cpu().double() @ v[0].T, x.cpu().double() @ v[1].T
+    h = torch.nn.functional.silu(a)
+    step = 2.0 ** -7
+    off = 1.05 * step * (1.1 * a.abs() * u.abs() + 2 * h.abs() * u.abs())
+    many, few = many.cpu().double(), few.cpu().double()
+    assert ((many - few).abs() <= 1.05 * (off @ v[2].abs().T + step * many.abs())).all()

@@ -132,6 +132,22 @@ def test_all_experts_of_one_and_many_experts():
     check(20, 96, 40, 512, 8, 0, seed=4)
 
 
+@pytest.mark.parametrize("tokens, experts, top", [(64, 384, 16), (48, 512, 16), (1, 512, 16), (64, 1, 1)])
+def test_the_limits_of_tokens_and_experts(tokens, experts, top):
+    check(tokens, 72, 40, experts, top, 0, seed=tokens)
+
+
+def test_rows_that_do_not_fit_are_refused():
+    E = enec()
+    for hidden, inter in ((20000, 64), (64, 20000)):
+        x, router = torch.zeros(1, hidden, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, hidden, dtype=torch.bfloat16, device="cuda")
+        streams = [torch.zeros(E.enec_microscaled_size(1, r, c), dtype=torch.uint8, device="cuda") for r, c in ((inter, hidden),) * 2 + ((hidden, inter),)]
+        y = torch.full((1, hidden), 5.0, dtype=torch.bfloat16, device="cuda")
+        assert call(E, x, router, streams, inter, 1, True, 0, y, hidden) == -8
+        torch.cuda.synchronize()
+        assert (y == 5).all()
+
+
 def test_long_rows():
     """Rows of which eight do not fit beside one another: smaller groups, both in front of and behind the activation."""
     check(16, 9000, 64, 2, 1, 0)
