@@ -124,7 +124,8 @@ enec_status launch(FewJob job, const MicroDevice& dev, cudaStream_t stream) {
     if (job.cluster == 0) return ENEC_ERR_TOO_LARGE;
     static std::atomic<uint64_t> allowed{0};
     if (!allow_shared(allowed, dev, enec_micro_few_kernel<DT>, kFewMostShared)) return ENEC_ERR_CUDA;
-    const uint32_t places = uint32_t(dev.sms) / job.cluster;
+    uint32_t places = uint32_t(dev.sms);
+    if (job.cluster > 1 && !resident_clusters(enec_micro_few_kernel<DT>, dev, job.cluster, kPieceThreads, bytes, places)) return ENEC_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((job.s.row_tiles < places ? job.s.row_tiles : places) * job.cluster);
     cfg.blockDim = dim3(kPieceThreads);

@@ -14,7 +14,6 @@
 
 #include <cooperative_groups.h>
 
-#include <mutex>
 
 #include "enec_micro_launch.cuh"
 
@@ -504,41 +503,6 @@ bool choose_group(uint32_t fixed, uint32_t records, uint32_t most, uint32_t leas
     return false;
 }
 
-// Clusters of a kernel that run at the same time, asked once per kernel, device and size; the last 32 answers are kept.
-template <class Kernel>
-bool resident_clusters(Kernel* kernel, const MicroDevice& dev, uint32_t bytes, uint32_t& out) {
-    struct Answer {
-        Kernel* kernel;
-        int ordinal;
-        uint32_t bytes;
-        int clusters;
-    };
-    static std::mutex mu;
-    static Answer known[32] = {};
-    static uint32_t next = 0;
-    std::lock_guard<std::mutex> lock(mu);
-    for (const Answer& a : known) {
-        if (a.kernel != kernel || a.ordinal != dev.ordinal || a.bytes != bytes) continue;
-        out = uint32_t(a.clusters);
-        return true;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kMoeCluster);
-    cfg.blockDim = dim3(kPieceThreads);
-    cfg.dynamicSmemBytes = bytes;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kMoeCluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) return false;
-    known[next++ % 32] = Answer{kernel, dev.ordinal, bytes, n};
-    out = uint32_t(n);
-    return true;
-}
-
 template <int DT>
 enec_status launch_moe(MoeJob job, const MicroDevice& dev, cudaStream_t stream) {
     const uint32_t pairs = job.tokens * job.top, tables = routing_bytes(pairs, job.experts);
@@ -557,7 +521,7 @@ enec_status launch_moe(MoeJob job, const MicroDevice& dev, cudaStream_t stream) 
         return ENEC_ERR_TOO_LARGE;
     if (!allow_shared(allowed_in, dev, enec_moe_in_kernel<DT>, kFewMostShared) ||
         !allow_shared(allowed_out, dev, enec_moe_out_kernel<DT>, kFewMostShared) ||
-        !resident_clusters(enec_moe_in_kernel<DT>, dev, bytes, clusters))
+        !resident_clusters(enec_moe_in_kernel<DT>, dev, kMoeCluster, kPieceThreads, bytes, clusters))
         return ENEC_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(clusters * kMoeCluster);
