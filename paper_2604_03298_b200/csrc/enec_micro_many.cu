@@ -22,13 +22,30 @@
 namespace enec {
 namespace {
 
-// Warps: bulk copies, matrix instructions, 8 for x, and 8 for each 128 rows of weights and results (half of them: 2048 x 4096 x 4096 took
-// 74 us, most of it the latency of bringing a step's weights back with two warps to a scheduler).
-constexpr uint32_t kFirstX = 2, kFirstW = 10, kThreadsX = 8 * 32;
-template <int MT>
-__host__ __device__ constexpr uint32_t many_threads() { return (kFirstW + 8 * MT) * 32; }
-// Stages of 128 rows x 64 columns of weights; of the tokens x 64 columns of x, at least and at most; of raw records, at most, as many as fit.
-constexpr uint32_t kStagesA = 5, kLeastB = 3, kMostB = 10, kMostRaw = 4;
+// Stages of x and of raw records at most, as many as fit.
+constexpr uint32_t kMostB = 12, kMostRaw = 4;
+
+// Who does what. 256 rows are bound by shared memory and the tensor cores; 128 rows with fewer tokens by how long a step takes one warp from
+// its first wait to its last arrival, some 900 clocks both for the warp that issues and for the eight that bring weights back. So
+// there two warps issue, each every other step to sums of its own that are added at the end, and four groups of warps bring back
+// every fourth step each, a thread a whole row of it. Either alone gains nothing; both: 64 tokens x 14336 x 4096 32.7 -> 23.4 us, four
+// issuing warps the same. Where x comes through registers a thread needs 80 of them, which leaves room for two groups: 128
+// tokens x 1411 x 2055 take 20 us so, with four groups 27.
+template <int MT, bool MAP>
+struct ManyShape {
+    static constexpr uint32_t kIssuers = MT == 1 ? 2 : 1;
+    static constexpr uint32_t kX = MAP ? 1 : 8;                          // warps for x
+    static constexpr uint32_t kParts = MT == 1 ? 1 : 2;                  // threads that share a row of a step
+    static constexpr uint32_t kGroups = MT == 2 ? 1 : MAP ? 4 : 2;       // of warps for the weights
+    static constexpr uint32_t kWeights = 128 * MT * kParts * kGroups;    // threads
+    static constexpr uint32_t kFirstX = 1 + kIssuers, kFirstW = kFirstX + kX, kThreads = kFirstW * 32 + kWeights;
+    // Stages of weights. A barrier answers for its last phase alone, and a warp that asks for a stage's next use must not be told of the use
+    // before: with several issuers or groups a stage, of weights or of x, always belongs to the same ones. A constant: counted at
+    // run time the issuing warp is slower by a tenth of the whole at 256 rows.
+    static constexpr uint32_t kStagesA = MT == 1 ? 4 : 5, kLeastB = MT == 1 ? 4 : 3;
+    static_assert(MT == 2 || (kStagesA % kIssuers == 0 && kStagesA % kGroups == 0 && kLeastB % kIssuers == 0), "");
+};
+
 constexpr uint32_t kManyMostTokens = 256;
 
 struct ManyJob {
@@ -44,14 +61,13 @@ struct ManyJob {
     uint32_t cluster;        // CTAs that share a tile's columns
     uint32_t share;          // records of columns each takes
     uint32_t stages_b, stages_raw;
-    uint32_t aligned;        // rows of x begin on 16-byte boundaries: tiles of it come by the tensor map
-    CUtensorMap map;
+    CUtensorMap map;         // of x, where its rows begin on 16-byte boundaries
     int* status;
 };
 
-template <int MT>
-__host__ __device__ constexpr uint32_t many_bytes(uint32_t tokens, uint32_t stages_b, uint32_t stages_raw) {
-    return stages_raw * MT * kMicroRecordBytes + kStagesA * 16384 + stages_b * tokens * 128 + 1024;
+template <int MT, bool MAP>
+uint32_t many_bytes(const ManyJob& job) {
+    return job.stages_raw * MT * kMicroRecordBytes + ManyShape<MT, MAP>::kStagesA * 16384 + job.stages_b * job.tile_tokens * 128 + 1024;
 }
 
 // 64 columns x tile_tokens rows of x from (column, token) on; zeros behind the matrix.
@@ -94,8 +110,10 @@ __device__ __forceinline__ uint4 to_values(uint32_t codes, uint32_t factor) {
     }
 }
 
-template <int DT, int MT>
-__global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(const __grid_constant__ ManyJob job) {
+template <int DT, int MT, bool MAP>
+__global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_many_kernel(const __grid_constant__ ManyJob job) {
+    using Shape = ManyShape<MT, MAP>;
+    constexpr uint32_t kStagesA = Shape::kStagesA;
     extern __shared__ uint8_t raw_shared[];
     __shared__ uint64_t raw_full[kMostRaw], raw_empty[kMostRaw], full_a[kStagesA], empty_a[kStagesA], full_b[kMostB], empty_b[kMostB], done;
     __shared__ uint32_t tmem_at;
@@ -103,13 +121,15 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t* smem = raw_shared + ((1024 - (smem_u32(raw_shared) & 1023)) & 1023);
     const uint32_t n = job.tile_tokens;
+    constexpr uint32_t kFirstX = Shape::kFirstX, kFirstW = Shape::kFirstW, kGroups = Shape::kGroups, kParts = Shape::kParts, kIssuers = Shape::kIssuers;
+    constexpr uint32_t kMine = 4 / kGroups, kEach = 2 / kParts;   // steps of a record, scales of a step's row
     uint32_t tmem_columns = 32;
-    while (tmem_columns < MT * n) tmem_columns *= 2;
+    while (tmem_columns < 2 * n) tmem_columns *= 2;
     if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < job.stages_raw; ++i) mbar_init(raw_full + i, 1), mbar_init(raw_empty + i, 8 * MT);
-        for (uint32_t i = 0; i < kStagesA; ++i) mbar_init(full_a + i, 8), mbar_init(empty_a + i, 1);
-        for (uint32_t i = 0; i < job.stages_b; ++i) mbar_init(full_b + i, job.aligned ? 1 : kThreadsX / 32), mbar_init(empty_b + i, 1);
-        mbar_init(&done, 1);
+        for (uint32_t i = 0; i < job.stages_raw; ++i) mbar_init(raw_full + i, 1), mbar_init(raw_empty + i, Shape::kWeights / 32);
+        for (uint32_t i = 0; i < kStagesA; ++i) mbar_init(full_a + i, 4 * kParts), mbar_init(empty_a + i, 1);
+        for (uint32_t i = 0; i < job.stages_b; ++i) mbar_init(full_b + i, Shape::kX), mbar_init(empty_b + i, 1);
+        mbar_init(&done, kIssuers);
         mbar_fence_init();
         failed = 0;
     }
@@ -153,28 +173,28 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
         // nothing may be in flight when the CTA ends
         for (uint32_t i = k > job.stages_raw ? k - job.stages_raw : 0; i < k; ++i)
             mbar_wait_bounded(raw_full + i % job.stages_raw, (i / job.stages_raw) & 1);
-    } else if (warp == 1) {
-        const uint32_t idesc = idesc_16bit(DT == ENEC_BF16, n);
+    } else if (warp < kFirstX) {
+        const uint32_t idesc = idesc_16bit(DT == ENEC_BF16, n), me = kIssuers == 1 ? 0 : warp - 1;
         const uint64_t a0 = operand_desc(smem_u32(a_ring)), b0 = operand_desc(smem_u32(b_ring));
-        uint32_t slot = 0, phase = 0, sb = 0, phase_b = 0;
-        uint32_t a_there = mbar_complete(full_a, 0), b_there = mbar_complete(full_b, 0);
+        uint32_t slot = me, phase = 0, sb = me, phase_b = 0;
+        uint32_t a_there = mbar_complete(full_a + slot, 0), b_there = mbar_complete(full_b + sb, 0);
         bool there = true;
-        for (uint32_t j = 0; j < steps && there; ++j) {
+        for (uint32_t j = me; j < steps && there; j += kIssuers) {
             const uint32_t sb_now = sb;
             const uint64_t b = b0 + sb * n * 8;
             there = b_there || suspended_wait(full_b + sb, phase_b, &failed);
-            if (++sb == job.stages_b) sb = 0, phase_b ^= 1;
+            if ((sb += kIssuers) >= job.stages_b) sb -= job.stages_b, phase_b ^= 1;
             b_there = mbar_complete(full_b + sb, phase_b);
             for (uint32_t i = 0; i < mt && there; ++i) {
                 const uint32_t now = slot;
                 const uint64_t a = a0 + slot * 1024;
                 there = a_there || suspended_wait(full_a + slot, phase, &failed);
-                if (++slot == kStagesA) slot = 0, phase ^= 1;
+                if ((slot += kIssuers) >= kStagesA) slot -= kStagesA, phase ^= 1;
                 a_there = mbar_complete(full_a + slot, phase);
                 if (!there) break;
                 tcgen05_fence_after();
 #pragma unroll
-                for (uint32_t q = 0; q < 4; ++q) mma_16bit(leader, tmem + i * n, a + q * 2, b + q * 2, idesc, j > 0 || q > 0);
+                for (uint32_t q = 0; q < 4; ++q) mma_16bit(leader, tmem + (me + i) * n, a + q * 2, b + q * 2, idesc, j > me || q > 0);
                 tcgen05_commit(leader, empty_a + now);
             }
             if (there) tcgen05_commit(leader, empty_b + sb_now);
@@ -189,8 +209,8 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
         const uint32_t first_col = min(k0 * kMicroCols, job.s.cols);
         const uint8_t* from = job.x + (uint64_t(token0) * job.ld_x + first_col) * 2;
         bool ok = true;
-        if (job.aligned) {
-            for (uint32_t j = 0; j < steps && warp == kFirstX; ++j) {
+        if constexpr (MAP) {
+            for (uint32_t j = 0; j < steps; ++j) {
                 if (j >= job.stages_b && !suspended_wait(empty_b + sb, phase, &failed)) {
                     ok = false;
                     break;
@@ -249,7 +269,7 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
         if (!ok) failed = 1;
     } else {
         // the weights: thread (tile, half, row) brings back 32 of the 64 columns of a step
-        const uint32_t me = threadIdx.x - kFirstW * 32, r = me & 127, half = me >> 7 & 1, i = me >> 8;
+        const uint32_t me = threadIdx.x - kFirstW * 32, r = me & 127, half = MT == 2 ? me >> 7 & 1 : 0, i = MT == 2 ? me >> 8 : 0, group = MT == 2 ? 0 : me >> 7;
         const bool mine = i < mt;   // the same for a warp
         uint32_t top = 0;
         if constexpr (DT == ENEC_FP16) {
@@ -264,23 +284,26 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
             }
             top = max(max(top & 255, top >> 8 & 255), max(top >> 16 & 255, top >> 24));
         }
-        const uint32_t a_base = smem_u32(a_ring) + r * 128, shift = 8 * half;
-        uint32_t place[4];   // of the four chunks of eight values in the operand's row
+        const uint32_t a_base = smem_u32(a_ring) + r * 128;
+        uint32_t place[4 * kEach];   // of the four chunks of eight values in the operand's row
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) place[e] = ((4 * half + e) ^ (r & 7)) << 4;
+        for (uint32_t e = 0; e < 4 * kEach; ++e) place[e] = ((4 * half + e) ^ (r & 7)) << 4;
         bool ok = true;
-        uint32_t s = 0, phase = 0;
+        uint32_t s = 0, phase = 0, sa = MT == 1 ? group : i, phase_a = 1;
         for (uint32_t k = 0; k < records && ok; ++k) {
             if (!suspended_wait(raw_full + s, phase, &failed)) {
                 ok = false;
                 break;
             }
-            uint4 codes[4];
+            uint4 codes[kMine][kEach];
             uint2 scales = {};   // eight bytes
             const uint32_t rec = smem_u32(raw) + (s * MT + i) * kMicroRecordBytes;
             if (mine) {
 #pragma unroll
-                for (uint32_t q = 0; q < 4; ++q) codes[q] = lds128(rec + r * 128 + (((2 * q + half) ^ (r & 7)) << 4));
+                for (uint32_t p = 0; p < kMine; ++p)
+#pragma unroll
+                    for (uint32_t h = 0; h < kEach; ++h)
+                        codes[p][h] = lds128(rec + r * 128 + (((2 * (p * kGroups + group) + half + h) ^ (r & 7)) << 4));
                 const uint32_t at = rec + kMicroElemBytes + (r & 31) * 16 + (r >> 5) * 4;
                 scales = make_uint2(lds32(at), lds32(at + 512));
             }
@@ -288,31 +311,36 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
             if (++s == job.stages_raw) s = 0, phase ^= 1;
             const uint32_t here = min(4u, steps - 4 * k);
 #pragma unroll
-            for (uint32_t q = 0; q < 4; ++q) {
+            for (uint32_t p = 0; p < kMine; ++p) {
+                const uint32_t q = p * kGroups + group;
                 if (q >= here) break;
                 if (mine) {
-                    const uint32_t use = (4 * k + q) * mt + i, sa = use % kStagesA;
-                    if (use >= kStagesA && !suspended_wait(empty_a + sa, (use / kStagesA - 1) & 1, &failed)) {
+                    const uint32_t at = sa;
+                    if (!suspended_wait(empty_a + at, phase_a, &failed)) {
                         ok = false;
                         break;
                     }
-                    const uint32_t byte = (q < 2 ? scales.x : scales.y) >> (16 * (q & 1) + shift) & 255;
-                    const uint32_t dst = a_base + sa * 16384;
-                    const uint32_t w[4] = {codes[q].x, codes[q].y, codes[q].z, codes[q].w};
-                    const uint32_t factor = DT == ENEC_BF16 ? bf16_factor(byte) : fp16_factor(byte, top);
-                    if (DT == ENEC_BF16 && __any_sync(0xFFFFFFFFu, byte > 142 && byte < 255)) {
-                        const uint32_t more = bf16_more(byte);
+                    const uint32_t dst = a_base + at * 16384, two = (q < 2 ? scales.x : scales.y) >> (16 * (q & 1));
 #pragma unroll
-                        for (uint32_t e = 0; e < 4; ++e) {
-                            const uint4 v = to_values<DT>(w[e], factor);
-                            sts128(dst + place[e], make_uint4(bf16_times(v.x, more), bf16_times(v.y, more), bf16_times(v.z, more), bf16_times(v.w, more)));
+                    for (uint32_t h = 0; h < kEach; ++h) {
+                        const uint32_t byte = two >> (8 * (half + h)) & 255;
+                        const uint32_t w[4] = {codes[p][h].x, codes[p][h].y, codes[p][h].z, codes[p][h].w};
+                        const uint32_t factor = DT == ENEC_BF16 ? bf16_factor(byte) : fp16_factor(byte, top);
+                        if (DT == ENEC_BF16 && __any_sync(0xFFFFFFFFu, byte > 142 && byte < 255)) {
+                            const uint32_t more = bf16_more(byte);
+#pragma unroll
+                            for (uint32_t e = 0; e < 4; ++e) {
+                                const uint4 v = to_values<DT>(w[e], factor);
+                                sts128(dst + place[4 * h + e], make_uint4(bf16_times(v.x, more), bf16_times(v.y, more), bf16_times(v.z, more), bf16_times(v.w, more)));
+                            }
+                        } else {
+#pragma unroll
+                            for (uint32_t e = 0; e < 4; ++e) sts128(dst + place[4 * h + e], to_values<DT>(w[e], factor));
                         }
-                    } else {
-#pragma unroll
-                        for (uint32_t e = 0; e < 4; ++e) sts128(dst + place[e], to_values<DT>(w[e], factor));
                     }
                     fence_async_shared();
-                    warp_arrive(full_a + sa);
+                    warp_arrive(full_a + at);
+                    if ((sa += MT == 1 ? kGroups : mt) >= kStagesA) sa -= kStagesA, phase_a ^= 1;
                 }
             }
         }
@@ -325,18 +353,25 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
         if constexpr (DT == ENEC_FP16) {
             // the rows' exponents change hands through shared memory that no operand uses any more
             uint8_t* tops = smem;
-            asm volatile("bar.sync 1, %0;" ::"n"(256 * MT) : "memory");
-            if (half == 0) tops[i * 128 + r] = uint8_t(top);
-            asm volatile("bar.sync 1, %0;" ::"n"(256 * MT) : "memory");
+            asm volatile("bar.sync 1, %0;" ::"n"(Shape::kWeights) : "memory");
+            if (half == 0 && group == 0) tops[i * 128 + r] = uint8_t(top);
+            asm volatile("bar.sync 1, %0;" ::"n"(Shape::kWeights) : "memory");
             factor = micro_scale(tops[i * 128 + row_in]);
-            asm volatile("bar.sync 1, %0;" ::"n"(256 * MT) : "memory");
+            asm volatile("bar.sync 1, %0;" ::"n"(Shape::kWeights) : "memory");
         }
         if (!failed && steps > 0 && mine) {
-            for (uint32_t c = half * 16; c < n; c += 32) {
+            for (uint32_t c = (MT == 2 ? half : group) * 16; c < n; c += 16 * kGroups * kParts) {
                 if (token0 + c >= job.tokens) break;
                 uint32_t v[16];
                 tmem_load16(tmem + (quarter * 32 << 16) + i * n + c, v);
                 tmem_load_wait();
+                for (uint32_t o = 1; MT == 1 && o < kIssuers && o < steps; ++o) {
+                    uint32_t other[16];
+                    tmem_load16(tmem + (quarter * 32 << 16) + o * n + c, other);
+                    tmem_load_wait();
+#pragma unroll
+                    for (uint32_t e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + __uint_as_float(other[e]));
+                }
                 if (MT == 1 && job.cluster > 1) {
                     float* sums = reinterpret_cast<float*>(smem);   // [token][row]
 #pragma unroll
@@ -379,20 +414,27 @@ __global__ void __launch_bounds__(many_threads<MT>(), 1) enec_micro_many_kernel(
     }
 }
 
-template <int DT, int MT>
+template <int DT, int MT, bool MAP>
 enec_status launch_many(ManyJob job, uint32_t tiles, const MicroDevice& dev, cudaStream_t stream) {
     static std::atomic<uint64_t> allowed{0};
-    if (!allow_shared(allowed, dev, enec_micro_many_kernel<DT, MT>, kFewMostShared)) return ENEC_ERR_CUDA;
-    // raw records first, then x, as far as there is room
-    job.stages_b = kLeastB, job.stages_raw = 1;
-    while (job.stages_raw < kMostRaw && many_bytes<MT>(job.tile_tokens, job.stages_b, job.stages_raw + 1) <= kFewMostShared) ++job.stages_raw;
-    while (job.stages_b < kMostB && many_bytes<MT>(job.tile_tokens, job.stages_b + 1, job.stages_raw) <= kFewMostShared) ++job.stages_b;
+    if (!allow_shared(allowed, dev, enec_micro_many_kernel<DT, MT, MAP>, kFewMostShared)) return ENEC_ERR_CUDA;
+    // x first, then raw records: a stage of x comes from L2 a step at a time, a record is taken to registers at once
+    using Shape = ManyShape<MT, MAP>;
+    job.stages_b = Shape::kLeastB, job.stages_raw = 1;
+    const auto grow = [&](uint32_t ManyJob::*stages, uint32_t by, uint32_t most) {
+        for (ManyJob more = job; (more.*stages += by) <= most && many_bytes<MT, MAP>(more) <= kFewMostShared;) job = more;
+    };
+    grow(&ManyJob::stages_raw, 1, 2);
+    grow(&ManyJob::stages_b, Shape::kIssuers, 6);
+    grow(&ManyJob::stages_raw, 1, 3);
+    grow(&ManyJob::stages_b, Shape::kIssuers, kMostB);
+    grow(&ManyJob::stages_raw, 1, kMostRaw);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(tiles * job.cluster);
-    cfg.blockDim = dim3(many_threads<MT>());
-    cfg.dynamicSmemBytes = many_bytes<MT>(job.tile_tokens, job.stages_b, job.stages_raw);
+    cfg.blockDim = dim3(Shape::kThreads);
+    cfg.dynamicSmemBytes = many_bytes<MT, MAP>(job);
     if (job.cluster > 1 && cfg.dynamicSmemBytes < job.tile_tokens * kMicroRows * 4 + 1024) cfg.dynamicSmemBytes = job.tile_tokens * kMicroRows * 4 + 1024;
-    const uint32_t least = MT * job.tile_tokens > 256 ? kTmemAloneShared : kTmemHalfShared;
+    const uint32_t least = 2 * job.tile_tokens > 256 ? kTmemAloneShared : kTmemHalfShared;
     if (cfg.dynamicSmemBytes < least) cfg.dynamicSmemBytes = least;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -403,7 +445,7 @@ enec_status launch_many(ManyJob job, uint32_t tiles, const MicroDevice& dev, cud
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = job.cluster > 1 ? 2 : 1;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, enec_micro_many_kernel<DT, MT>, job);
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, enec_micro_many_kernel<DT, MT, MAP>, job);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return err == cudaSuccess ? ENEC_OK : ENEC_ERR_CUDA;
 }
@@ -436,8 +478,8 @@ enec_status micro_many(const MicroProduct& p, const MicroDevice& dev, cudaStream
     const uint64_t token_tiles = (p.tokens + kManyMostTokens - 1) / kManyMostTokens;
     job.tile_tokens = uint32_t(((p.tokens + token_tiles - 1) / token_tiles + 15) / 16 * 16);
     // a map's stride is a multiple of 16 bytes and below 2^40
-    job.aligned = p.ld_x % 8 == 0;
-    if (job.aligned) {
+    const bool aligned = p.ld_x % 8 == 0;
+    if (aligned) {
         const cuuint64_t extent[2] = {p.s.cols, p.tokens}, stride[1] = {p.ld_x * 2};
         const cuuint32_t box[2] = {64, job.tile_tokens}, step[2] = {1, 1};
         const auto encode = map_encoder();
@@ -456,9 +498,18 @@ enec_status micro_many(const MicroProduct& p, const MicroDevice& dev, cudaStream
     if (mt == 1)
         while (job.cluster < 8 && tiles * job.cluster * 2 <= uint64_t(dev.sms) * 3 / 2 && p.s.col_tiles >= 4 * job.cluster) job.cluster *= 2;
     job.share = (p.s.col_tiles + job.cluster - 1) / job.cluster;
-    if (p.dt == ENEC_BF16)
-        return mt == 2 ? launch_many<ENEC_BF16, 2>(job, uint32_t(tiles), dev, stream) : launch_many<ENEC_BF16, 1>(job, uint32_t(tiles), dev, stream);
-    return mt == 2 ? launch_many<ENEC_FP16, 2>(job, uint32_t(tiles), dev, stream) : launch_many<ENEC_FP16, 1>(job, uint32_t(tiles), dev, stream);
+    const auto launch = [&](auto dt, auto tiles_high) {
+        constexpr int kDt = decltype(dt)::value, kMt = decltype(tiles_high)::value;
+        return aligned ? launch_many<kDt, kMt, true>(job, uint32_t(tiles), dev, stream) : launch_many<kDt, kMt, false>(job, uint32_t(tiles), dev, stream);
+    };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    if (p.dt == ENEC_BF16) {
+        const std::integral_constant<int, ENEC_BF16> dt;
+        return mt == 2 ? launch(dt, two) : launch(dt, one);
+    }
+    const std::integral_constant<int, ENEC_FP16> dt;
+    return mt == 2 ? launch(dt, two) : launch(dt, one);
 }
 
 }  // namespace enec

@@ -187,6 +187,16 @@ def test_product_of_many_tiles(dt, tokens, rows, cols, gap):
     check_product(tokens, rows, cols, dt, gap)
 
 
+# steps of 64 columns are shared out among warps that issue and warps that bring weights back: fewer steps than warps, odd
+# numbers of them, more than the stages hold
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("tokens", [17, 80, 144, 256])
+@pytest.mark.parametrize("cols", [8, 64, 72, 128, 192, 256, 320, 448, 832, 2112])
+def test_product_of_few_steps(dt, tokens, cols):
+    check_product(tokens, 150, cols, dt)
+    check_product(tokens, 150, cols, dt, 3)
+
+
 @pytest.mark.parametrize("dt", [0, 1])
 @pytest.mark.parametrize("tokens, rows, cols", [(8, 48, 14336), (32, 40, 14336), (3, 20, 60000), (1, 4096, 4096), (65, 20, 20000)])
 def test_product_of_long_rows(dt, tokens, rows, cols):
