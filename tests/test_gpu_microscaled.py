@@ -197,6 +197,12 @@ def test_product_of_few_steps(dt, tokens, cols):
     check_product(tokens, 150, cols, dt, 3)
 
 
+# the columns of a tile shared out: to 6 CTAs, to 4 since 16 times 8 would not run at once, to 7, 5 and 3; the last ones with less than the others
+@pytest.mark.parametrize("tokens, rows, cols", [(17, 1024, 4100), (100, 2048, 4096), (70, 300, 3400), (33, 640, 2300), (256, 5100, 1500)])
+def test_product_of_shared_columns(tokens, rows, cols):
+    check_product(tokens, rows, cols, 0)
+
+
 @pytest.mark.parametrize("dt", [0, 1])
 @pytest.mark.parametrize("tokens, rows, cols", [(8, 48, 14336), (32, 40, 14336), (3, 20, 60000), (1, 4096, 4096), (65, 20, 20000)])
 def test_product_of_long_rows(dt, tokens, rows, cols):
