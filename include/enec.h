@@ -237,8 +237,10 @@ enec_status enec_dequantize_microscaled(const void* d_in, size_t in_size, enec_d
 /*
  * y = x W^T: x [tokens, cols] and y [tokens, rows] of type dt (bf16 or fp16), W a stream of one matrix of rows x cols. Sums are in fp32,
  * y is rounded once, W not at all. Up to 16 tokens, a value of x counts to 2^-22 of the largest of the 32 neighbours (columns 32c ..) that
- * it stands among (and to 2^-127): beyond a bf16 value's last bit for all within 2^-14 of that largest one. With more tokens x is not
- * rounded either. A token with an infinity or a NaN has infinities or NaN in all of its results. From one token (bound by the weights' bytes) to
+ * it stands among (and to 2^-127), also where that largest one meets a weight of zero: beyond a bf16 value's last bit for all within 2^-14
+ * of it. With more tokens x is not rounded either; in fp16, rows of W whose blocks' scales lie more than 2^36 apart (blocks of zeros and
+ * of values below 2^-67 aside) then take up to 300 times as long as others. Weights of 2^128 and more, which only streams from elsewhere
+ * hold, may count as infinities. A token with an infinity or a NaN has infinities or NaN in all of its results. From one token (bound by the weights' bytes) to
  * thousands (bound by the tensor cores). tokens == 0 or rows == 0 is valid and does nothing; cols == 0 gives zeros. x and y must not overlap.
  */
 enec_status enec_matmul_microscaled(const void* d_x, enec_dtype dt, size_t tokens, size_t ld_x, const void* d_w, size_t w_size,

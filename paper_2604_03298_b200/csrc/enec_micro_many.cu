@@ -6,8 +6,11 @@
 // tiles of 128 x 256 would need twice that. Raw records are copied in bulk; a
 // thread takes its share of a record to registers at once, so that one record's room is enough.
 //
-// bf16: a code's value times its scale is exact in bf16 over the whole range of scales. fp16: it would not be, so a row's values are
-// held times 2^-(largest scale exponent of the row), and the sum is scaled back: what is lost lies under 2^-24 of the row's largest.
+// bf16: a code's value times its scale is exact in bf16 over the whole range of scales. fp16: it would not be, so a row's values are held
+// times 2^(13 - largest scale exponent of the row), and the sum is scaled back. fp16 has the values of blocks down to 2^-36 of the
+// row's largest so (3 x 2^14 to 2^-24). Blocks that cannot add up to 2^-37, far below fp16's last place, are not counted; rows
+// whose other blocks lie further apart take their sums again, in fp32 on the codes themselves (wide_row_sum): 2048 tokens x 4096 x 4096
+// take 62 us without such rows, 530 us with one in 128, 20 ms with nothing else.
 //
 // Where the tiles would not fill the SMs, a cluster of CTAs shares the columns: each leaves its sums in its shared memory and adds
 // up a part of the tokens, in the order of the CTAs.
@@ -49,6 +52,7 @@ struct ManyShape {
 };
 
 constexpr uint32_t kManyMostTokens = 256;
+constexpr uint32_t kFp16Up = 13, kFp16Span = 36;   // a row's largest scale becomes 2^13; the smallest that fp16 has all values of, below it
 
 struct ManyJob {
     const uint8_t* x;
@@ -89,12 +93,13 @@ __device__ __forceinline__ uint32_t fp16_times(uint32_t a, uint32_t b) {
 }
 
 // What 32 codes of a scale byte are multiplied with, in both halves of a word. bf16: the values come times 2^-112 (see to_values), so
-// 2^(byte - 15); scales above 2^15 need a second factor (bf16_more). fp16: 2^(byte - top), byte <= top. 255 is not a number.
+// 2^(byte - 15); scales above 2^15 need a second factor (bf16_more). fp16: 2^(13 + byte - top), 0 for scales that are not counted. 255 is
+// not a number.
 __device__ __forceinline__ uint32_t bf16_factor(uint32_t byte) { return (byte == 255 ? 0x7FC0u : (min(byte, 142u) + 112) << 7) * 0x10001u; }
 __device__ __forceinline__ uint32_t bf16_more(uint32_t byte) { return (byte > 142 && byte < 255 ? (byte - 142 + 127) << 7 : 0x3F80u) * 0x10001u; }
 __device__ __forceinline__ uint32_t fp16_factor(uint32_t byte, uint32_t top) {
-    const uint32_t below = top - byte;
-    return (byte == 255 ? 0x7E00u : below < 15 ? (15 - below) << 10 : below < 25 ? 0x400u >> (below - 14) : 0u) * 0x10001u;
+    const uint32_t below = top - byte;   // 2^32 less something where the whole row is not counted
+    return (byte == 255 ? 0x7E00u : below < 15 + kFp16Up ? (15 + kFp16Up - below) << 10 : below < 25 + kFp16Up ? 0x400u >> (below - 14 - kFp16Up) : 0u) * 0x10001u;
 }
 // Eight codes times a factor. fp16 holds a code's value with its exponent field in 14 .. 17 and at most one mantissa bit; for bf16 the same
 // fields three bits further down are the value times 2^-112.
@@ -110,6 +115,38 @@ __device__ __forceinline__ uint4 to_values(uint32_t codes, uint32_t factor) {
         h.w = select_bits(0x80008000u, h.w, (h.w >> 3) & 0x0FFF0FFFu);
         return make_uint4(bf16_times(h.x, factor), bf16_times(h.y, factor), bf16_times(h.z, factor), bf16_times(h.w, factor));
     }
+}
+
+// A warp: sums of one row of weights and 16 tokens, by lanes t and t + 16 that of token t. Every second block a lane: the sum of codes times
+// values, then times the block's scale. rec: the first record; row: in it; at: where the first token's values begin; valid_tokens: rows
+// of x that exist. Out of line: no ordinary weights come here, and the registers are the main loop's.
+__device__ __noinline__ float wide_row_sum(const uint8_t* rec, uint32_t row, uint32_t columns, const uint8_t* at, uint64_t ld_x, uint32_t valid_tokens) {
+    const uint32_t lane = threadIdx.x & 31, t = lane & 15;
+    const uint8_t* x = at + uint64_t(t) * ld_x * 2;
+    float sum = 0.f;
+    for (uint32_t c = lane >> 4; c * kMicroBlock < columns; c += 2) {
+        const uint8_t* r = rec + uint64_t(c >> 3) * kMicroRecordBytes;
+        const uint4 codes = __ldg(reinterpret_cast<const uint4*>(r + row * 128 + (((c & 7) ^ (row & 7)) << 4)));
+        const uint32_t scale = __ldg(r + kMicroElemBytes + (c >> 2 & 1) * 512 + (row & 31) * 16 + (row >> 5) * 4 + (c & 3));
+        const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+        float part = 0.f;
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+            const uint32_t col = c * kMicroBlock + e * 8;
+            uint32_t words[4];
+            load_eight<ENEC_FP16>(x + uint64_t(col) * 2, t < valid_tokens && col < columns ? int(min(columns - col, 8u)) : 0, words);
+            const uint4 h = e2m1_values(w[e]);
+            const uint32_t hw[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const float2 a = MicroType<ENEC_FP16>::unpack(hw[i]), b = MicroType<ENEC_FP16>::unpack(words[i]);
+                part = fmaf(a.x, b.x, part);
+                part = fmaf(a.y, b.y, part);
+            }
+        }
+        sum = fmaf(part, micro_scale(scale), sum);
+    }
+    return sum + __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
 }
 
 template <int DT, int MT, bool MAP>
@@ -274,17 +311,33 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
         const uint32_t me = threadIdx.x - kFirstW * 32, r = me & 127, half = MT == 2 ? me >> 7 & 1 : 0, i = MT == 2 ? me >> 8 : 0, group = MT == 2 ? 0 : me >> 7;
         const bool mine = i < mt;   // the same for a warp
         uint32_t top = 0;
+        bool wide = false;
         if constexpr (DT == ENEC_FP16) {
-            // the largest of the row's scale bytes, four at a time; 255 does not count
+            // The largest and the smallest of the row's scale bytes. 255 does not count, and neither do bytes up to 71 - log2 of the
+            // columns, rounded up: such weights are below 2^2.6 2^(71 - 127) / columns and values of x below 2^16, so all of them
+            // together are below 2^-37, where half of fp16's smallest step is 2^-25. (Blocks of zeros have the byte 0.)
+            // Two bytes at a time, as (byte + 1) mod 256 + up: those that count become 256 and more, exclusive-or 256 less than the others.
+            const uint32_t none = 71 - (32 - __clz(job.s.cols - 1)), up = (254 - none) * 0x10001u;
             const uint8_t* at = wr + i * strip + kMicroElemBytes + (r & 31) * 16 + (r >> 5) * 4;
+            uint32_t high = 0, low = 0xFFFFFFFFu;
             if (mine) {
 #pragma unroll 8
                 for (uint32_t b = 0; b < 2 * records; ++b) {
                     const uint32_t four = __ldg(reinterpret_cast<const uint32_t*>(at + uint64_t(b >> 1) * kMicroRecordBytes + (b & 1) * 512));
-                    top = __vmaxu4(top, four & ~__vcmpeq4(four, 0xFFFFFFFFu));
+#pragma unroll
+                    for (uint32_t e = 0; e < 2; ++e) {
+                        const uint32_t two = (((four >> (8 * e) & 0x00FF00FFu) + 0x00010001u) & 0x00FF00FFu) + up;
+                        high = __vmaxu2(high, two);
+                        low = __vminu2(low, two ^ 0x01000100u);
+                    }
                 }
             }
-            top = max(max(top & 255, top >> 8 & 255), max(top >> 16 & 255, top >> 24));
+            high = max(high & 0xFFFF, high >> 16), low = min(low & 0xFFFF, low >> 16);
+            if (high >= 256) {
+                wide = high - 256 > low + kFp16Span;
+                top = high - 255 + none;
+            }
+            top = max(top, kFp16Up);
         }
         const uint32_t a_base = smem_u32(a_ring) + r * 128;
         uint32_t place[4 * kEach];   // of the four chunks of eight values in the operand's row
@@ -352,13 +405,15 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
         // results: the warp's quarter of the lanes, every other 16 tokens of its tile
         const uint32_t quarter = warp & 3, row_in = quarter * 32 + lane, row = (row_tile + i) * kMicroRows + row_in;
         float factor = 1.f;
+        uint32_t wide_rows = 0;   // of the warp's 32
         if constexpr (DT == ENEC_FP16) {
             // the rows' exponents change hands through shared memory that no operand uses any more
-            uint8_t* tops = smem;
+            uint16_t* tops = reinterpret_cast<uint16_t*>(smem);
             asm volatile("bar.sync 1, %0;" ::"n"(Shape::kWeights) : "memory");
-            if (half == 0 && group == 0) tops[i * 128 + r] = uint8_t(top);
+            if (half == 0 && group == 0) tops[i * 128 + r] = uint16_t((top - kFp16Up) << 1 | uint32_t(wide));
             asm volatile("bar.sync 1, %0;" ::"n"(Shape::kWeights) : "memory");
-            factor = micro_scale(tops[i * 128 + row_in]);
+            factor = micro_scale(tops[i * 128 + row_in] >> 1);
+            wide_rows = __ballot_sync(0xFFFFFFFFu, row < job.s.rows && (tops[i * 128 + row_in] & 1));
             asm volatile("bar.sync 1, %0;" ::"n"(Shape::kWeights) : "memory");
         }
         if (!failed && steps > 0 && mine) {
@@ -380,6 +435,19 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
                     for (uint32_t e = 0; e < 16; ++e) sums[(c + e) * kMicroRows + row_in] = __uint_as_float(v[e]) * factor;
                 } else if (good) {
                     store_tile16<DT>(job.y, job.ld_y, token0 + c, job.tokens, row, job.s.rows, v, factor, lane);
+                }
+                if constexpr (DT == ENEC_FP16) {
+                    // over what this warp's lanes have just stored
+                    if (wide_rows) __syncwarp();
+                    for (uint32_t left = wide_rows; left; left &= left - 1) {
+                        const uint32_t r_wide = quarter * 32 + __ffs(left) - 1, t = lane & 15;
+                        const float sum = wide_row_sum(wr + i * strip, r_wide, columns, job.x + (uint64_t(token0 + c) * job.ld_x + k0 * kMicroCols) * 2,
+                                                       job.ld_x, job.tokens - token0 - c);
+                        if (lane >= 16) continue;
+                        if (MT == 1 && job.cluster > 1) reinterpret_cast<float*>(smem)[(c + t) * kMicroRows + r_wide] = sum;
+                        else if (good && token0 + c + t < job.tokens)
+                            reinterpret_cast<__half*>(job.y)[uint64_t(token0 + c + t) * job.ld_y + row - row_in + r_wide] = __float2half_rn(sum);
+                    }
                 }
             }
         }
