@@ -199,7 +199,8 @@ extern "C" enec_status enec_matmul_microscaled_both(const void* d_x, size_t x_si
     if (!d_x || !d_w || !d_y || !micro_aligned16(d_x) || !micro_aligned16(d_w) || !micro_aligned16(d_y) || ld_y < rows || (uint64_t(ld_y) >> 36))
         return ENEC_ERR_INVALID_ARG;
     if (x_size < job.sx.total || w_size < job.sw.total) return ENEC_ERR_BUFFER_TOO_SMALL;
-    if (cols == 0) return cudaMemset2DAsync(d_y, ld_y * 2, 0, rows * 2, tokens, stream) == cudaSuccess ? ENEC_OK : ENEC_ERR_CUDA;
+    if (cols == 0)
+        return micro_no_columns(static_cast<const uint8_t*>(d_x), job.sx, static_cast<const uint8_t*>(d_w), job.sw, tokens, d_y, ld_y, d_status, stream);
     MicroDevice dev;
     if (!micro_device(dev)) return ENEC_ERR_CUDA;
     job.x = static_cast<const uint8_t*>(d_x);

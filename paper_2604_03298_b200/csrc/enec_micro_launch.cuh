@@ -60,6 +60,9 @@ constexpr uint32_t kFewMostShared = 226 * 1024;   // the kernels have a little s
 // Whether the form for few tokens takes a call (up to 16 tokens, as long as their digits fit into a cluster's shared memory).
 bool micro_few_takes(uint32_t tokens, uint32_t col_tiles);
 enec_status micro_few(const MicroProduct& p, const MicroDevice& dev, cudaStream_t stream);
+// Products of no columns: zeros, if the streams' headers say what the call says. x: null or a stream too.
+enec_status micro_no_columns(const uint8_t* x, const MicroShape& sx, const uint8_t* w, const MicroShape& sw, uint64_t tokens, void* y, uint64_t ld_y,
+                             int* status, cudaStream_t stream);
 // All tokens of the product, on the tensor cores.
 enec_status micro_many(const MicroProduct& p, const MicroDevice& dev, cudaStream_t stream);
 
