@@ -81,8 +81,10 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
             const uint8_t* wr = job.w + kMicroHeaderBytes + tile.row_tile * strip;
             const uint8_t* xr = job.x + kMicroHeaderBytes + tile.x_tile * strip;
             for (uint32_t k = 0; k < records; ++k, wr += kMicroRecordBytes, xr += kMicroRecordBytes) {
-                if (asked >= job.stages && !suspended_wait(empty + s, phase, &failed)) failed = 1;
-                if (failed) break;
+                if (asked >= job.stages && !warp_wait(empty + s, phase, &failed)) {
+                    failed = 1;
+                    break;
+                }
                 if (leader) {
                     uint8_t* a = smem + s * stage_bytes;
                     uint8_t* b = a + kMicroElemBytes;
@@ -140,6 +142,7 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
         }
         // no instruction may be under way when tensor memory is given back
         for (uint32_t k = i > 2 ? i - 2 : 0; k < i; ++k) mbar_wait_bounded(done + (k & 1), (k >> 1) & 1);
+        __syncwarp();
     } else {
         const MicroProbe w_header(job.w), x_header(job.x);
         const bool good = w_header.fits(job.sw) && x_header.fits(job.sx);
@@ -148,9 +151,9 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
         for (uint32_t t = blockIdx.x; t < job.tiles; t += gridDim.x, ++i) {
             const BothTile tile(job, t);
             const uint32_t set = i & 1, row = tile.row_tile * kMicroRows + quarter * 32 + lane;
-            if (!suspended_wait(done + set, (i >> 1) & 1, &failed)) failed = 1;
+            if (!warp_wait(done + set, (i >> 1) & 1, &failed)) failed = 1;
             tcgen05_fence_after();
-            if (good && !failed) {
+            if (good && !warp_failed(&failed)) {
                 for (uint32_t c = half * 16; c < n; c += 32) {
                     if (tile.token0 + c >= job.sx.rows) break;
                     uint32_t v[16];

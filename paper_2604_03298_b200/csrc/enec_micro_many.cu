@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
     if (warp == 0) {
         uint32_t k = 0, s = 0, phase = 1;
         for (; k < records; ++k) {
-            if (k >= job.stages_raw && !suspended_wait(raw_empty + s, phase, &failed)) {
+            if (k >= job.stages_raw && !warp_wait(raw_empty + s, phase, &failed)) {
                 failed = 1;
                 break;
             }
@@ -241,17 +241,17 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
         if (!there) failed = 1;
         tcgen05_commit(leader, &done);
         mbar_wait_bounded(&done, 0);   // no instruction may be under way when tensor memory is given back
+        __syncwarp();
     } else if (warp < kFirstW) {
         // x: eight lanes a row of 64 columns
         const uint32_t me = threadIdx.x - kFirstX * 32, c = me & 7;
         uint32_t asked = 0, sb = 0, phase = 1;
         const uint32_t first_col = min(k0 * kMicroCols, job.s.cols);
         const uint8_t* from = job.x + (uint64_t(token0) * job.ld_x + first_col) * 2;
-        bool ok = true;
         if constexpr (MAP) {
             for (uint32_t j = 0; j < steps; ++j) {
-                if (j >= job.stages_b && !suspended_wait(empty_b + sb, phase, &failed)) {
-                    ok = false;
+                if (j >= job.stages_b && !warp_wait(empty_b + sb, phase, &failed)) {
+                    failed = 1;
                     break;
                 }
                 if (leader) {
@@ -280,15 +280,12 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
             };
 #pragma unroll
             for (uint32_t a = 0; a < kAhead; ++a) load(v[a], a);
-            for (uint32_t batch0 = 0; batch0 < all && ok; batch0 += kAhead) {
+            for (uint32_t batch0 = 0; batch0 < all; batch0 += kAhead) {
 #pragma unroll
                 for (uint32_t a = 0; a < kAhead; ++a) {
                     const uint32_t batch = batch0 + a, j = batch / batches, part = batch - j * batches;
-                    if (batch >= all || !ok) break;
-                    if (part == 0 && j >= job.stages_b && !suspended_wait(empty_b + sb, phase, &failed)) {
-                        ok = false;
-                        break;
-                    }
+                    if (batch >= all) break;
+                    if (part == 0 && j >= job.stages_b && !suspended_wait(empty_b + sb, phase, &failed)) failed = 1;
 #pragma unroll
                     for (uint32_t i = 0; i < 2; ++i) {
                         const uint32_t r = part * 64 + i * 32 + (me >> 3);
@@ -305,7 +302,6 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
                 }
             }
         }
-        if (!ok) failed = 1;
     } else {
         // the weights: thread (tile, half, row) brings back 32 of the 64 columns of a step
         const uint32_t me = threadIdx.x - kFirstW * 32, r = me & 127, half = MT == 2 ? me >> 7 & 1 : 0, i = MT == 2 ? me >> 8 : 0, group = MT == 2 ? 0 : me >> 7;
@@ -343,13 +339,9 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
         uint32_t place[4 * kEach];   // of the four chunks of eight values in the operand's row
 #pragma unroll
         for (uint32_t e = 0; e < 4 * kEach; ++e) place[e] = ((4 * half + e) ^ (r & 7)) << 4;
-        bool ok = true;
         uint32_t s = 0, phase = 0, sa = MT == 1 ? group : i, phase_a = 1;
-        for (uint32_t k = 0; k < records && ok; ++k) {
-            if (!suspended_wait(raw_full + s, phase, &failed)) {
-                ok = false;
-                break;
-            }
+        for (uint32_t k = 0; k < records; ++k) {
+            if (!suspended_wait(raw_full + s, phase, &failed)) failed = 1;
             uint4 codes[kMine][kEach];
             uint2 scales = {};   // eight bytes
             const uint32_t rec = smem_u32(raw) + (s * MT + i) * kMicroRecordBytes;
@@ -371,10 +363,7 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
                 if (q >= here) break;
                 if (mine) {
                     const uint32_t at = sa;
-                    if (!suspended_wait(empty_a + at, phase_a, &failed)) {
-                        ok = false;
-                        break;
-                    }
+                    if (!suspended_wait(empty_a + at, phase_a, &failed)) failed = 1;
                     const uint32_t dst = a_base + at * 16384, two = (q < 2 ? scales.x : scales.y) >> (16 * (q & 1));
 #pragma unroll
                     for (uint32_t h = 0; h < kEach; ++h) {
@@ -399,7 +388,6 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
                 }
             }
         }
-        if (!ok) failed = 1;
         if (!suspended_wait(&done, 0, &failed)) failed = 1;
         tcgen05_fence_after();
         // results: the warp's quarter of the lanes, every other 16 tokens of its tile
@@ -416,7 +404,7 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
             wide_rows = __ballot_sync(0xFFFFFFFFu, row < job.s.rows && (tops[i * 128 + row_in] & 1));
             asm volatile("bar.sync 1, %0;" ::"n"(Shape::kWeights) : "memory");
         }
-        if (!failed && steps > 0 && mine) {
+        if (!warp_failed(&failed) && steps > 0 && mine) {
             for (uint32_t c = (MT == 2 ? half : group) * 16; c < n; c += 16 * kGroups * kParts) {
                 if (token0 + c >= job.tokens) break;
                 uint32_t v[16];

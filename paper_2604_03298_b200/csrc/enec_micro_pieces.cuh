@@ -194,8 +194,8 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
         uint32_t asked = 0, slot = 0, phase = 0;
         for (uint32_t i = 0; i < n_tasks; ++i, tasks.next()) {
             const PieceTask task = tasks.get();
-            for (uint32_t k = 0; k < task.count && !sh.failed; ++k) {
-                if (asked >= stages && !suspended_wait(sh.empty + slot, phase ^ 1, &sh.failed)) {
+            for (uint32_t k = 0; k < task.count; ++k) {
+                if (asked >= stages && !warp_wait(sh.empty + slot, phase ^ 1, &sh.failed)) {
                     sh.failed = 1;
                     break;
                 }
@@ -262,10 +262,12 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
             }
             if (begins) flipped ^= (1u << sweeps.batches) - 1;
             tcgen05_commit(leader, sh.done + set);
+            __syncwarp();
             if (lockstep) meet(i);
         }
         // no instruction may be under way when tensor memory is given back
         for (uint32_t i = n_tasks > 2 ? n_tasks - 2 : 0; i < n_tasks; ++i) suspended_wait(sh.done + (i & 1), (i >> 1) & 1, &never);
+        __syncwarp();
     } else {
         uint32_t group = 0xFFFFFFFFu;
         for (uint32_t i = 0; i < n_tasks; ++i, tasks.next()) {
@@ -275,9 +277,9 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
                 stage_digits(sh, warp - 2, threadIdx.x & 31, task, digits, values);
             }
             const uint32_t set = i & 1;
-            if (!suspended_wait(sh.done + set, (i >> 1) & 1, &sh.failed)) sh.failed = 1;
+            if (!warp_wait(sh.done + set, (i >> 1) & 1, &sh.failed)) sh.failed = 1;
             tcgen05_fence_after();
-            const bool ok = !sh.failed;
+            const bool ok = !warp_failed(&sh.failed);
             take(i, tmem + set * (kPieceTokens * kPieces) + ((warp & 3) * 32 << 16), ok);
             tcgen05_fence_before();
             warp_arrive(sh.drained + set);
