@@ -263,7 +263,7 @@ enec_status enec_matmul_microscaled_both(const void* d_x, size_t x_size, size_t 
  * Sums are in fp32 and y is rounded once; x and the hidden values in fp32 count to 2^-22 of the largest of their 32 neighbours.
  * tokens <= 64, experts <= 512, top_k <= min(16, experts), tokens * experts <= 24576, else ENEC_ERR_TOO_LARGE or, for top_k beyond
  * experts and for sizes of zero, ENEC_ERR_INVALID_ARG; ENEC_ERR_TOO_LARGE too where not one token's row of hidden or inter values fits
- * into an SM's shared memory (about 12000 values). tokens == 0 is valid and does nothing.
+ * into an SM's shared memory (about 15000 values). tokens == 0 is valid and does nothing.
  * d_workspace: enec_moe_microscaled_workspace bytes of device memory, 16-byte aligned, of any content; the call uses it from its
  * beginning to its end, so calls that may overlap on the GPU need one each.
  */

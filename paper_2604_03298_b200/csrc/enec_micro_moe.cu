@@ -488,19 +488,23 @@ __global__ void __launch_bounds__(kPieceThreads, 1) enec_moe_out_kernel(const __
     }
 }
 
-// Pairs per group, stages of the ring and with them the shared memory: as many pairs as there may be with four stages.
+// Pairs per group, stages of the ring and with them the shared memory: as many pairs as there may be with four stages; where there is no room
+// for one pair so, with three or two.
 bool choose_group(uint32_t fixed, uint32_t records, uint32_t most, uint32_t least_bytes, uint32_t& group, uint32_t& stages, uint32_t& bytes) {
-    for (group = most; group > 0; --group) {
-        const uint64_t others = 1024 + fixed + uint64_t(records) * piece_record_bytes(group);
-        if (others + 4 * kMicroRecordBytes > kFewMostShared) continue;
+    const auto fits = [&](uint32_t pairs, uint32_t ring) {
+        const uint64_t others = 1024 + fixed + uint64_t(records) * piece_record_bytes(pairs);
+        if (others + ring * kMicroRecordBytes > kFewMostShared) return false;
         const uint64_t fit = (kFewMostShared - others) / kMicroRecordBytes;
+        group = pairs;
         stages = fit < kPieceMostStages ? uint32_t(fit) : kPieceMostStages;
         bytes = uint32_t(others + stages * kMicroRecordBytes);
         if (bytes < 1024 + fixed + least_bytes) bytes = 1024 + fixed + least_bytes;
         if (bytes < kTmemAloneShared) bytes = kTmemAloneShared;
         return bytes <= kFewMostShared;
-    }
-    return false;
+    };
+    for (uint32_t pairs = most; pairs > 0; --pairs)
+        if (fits(pairs, 4)) return true;
+    return fits(1, 2);
 }
 
 template <int DT>
