@@ -95,7 +95,14 @@ def lib():
     return _LIB
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream   # of a device, an integer
+def _raw_stream(device):
+    # a device's current stream as an integer; looked up at the first call, since a torch without CUDA has no such function and what
+    # needs no GPU (sizes, refusals) works there too
+    global _raw_stream
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+    return _raw_stream(device)
+
+
 _device = torch.cuda.current_device
 
 

@@ -123,3 +123,17 @@ def test_moe_workspace_holds_the_pairs_values(lib):
     for tokens, hidden, inter, experts, top in ((1, 1, 1, 1, 1), (4, 64, 32, 8, 2), (64, 2048, 1408, 64, 6)):
         pairs = tokens * top
         assert f(tokens, hidden, inter, experts, top) >= pairs * (hidden + inter) * 4 + pairs * 8
+
+
+def test_import_and_host_functions_without_a_torch_for_cuda():
+    """A torch built without CUDA has no raw streams: the package is importable there, and what only the host computes works."""
+    import os
+    import subprocess
+    import sys
+    code = ("import torch\n"
+            "del torch._C._cuda_getCurrentRawStream\n"
+            "import paper_2604_03298_b200 as E\n"
+            "assert E.enec_microscaled_size(1, 128, 256) == 128 + 17408 and E.enec_max_compressed_size(0, 1 << 20) > 0\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert run.returncode == 0, run.stderr
