@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kBothThreads, 1) enec_micro_both_kernel(const 
         for (uint32_t t = blockIdx.x; t < job.tiles; t += gridDim.x, ++i) {
             const BothTile tile(job, t);
             const uint32_t set = i & 1, row = tile.row_tile * kMicroRows + quarter * 32 + lane;
-            if (!warp_wait(done + set, (i >> 1) & 1, &failed)) failed = 1;
+            wait_or_fail(done + set, (i >> 1) & 1, &failed);
             tcgen05_fence_after();
             if (good && !warp_failed(&failed)) {
                 for (uint32_t c = half * 16; c < n; c += 32) {

@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
                 for (uint32_t a = 0; a < kAhead; ++a) {
                     const uint32_t batch = batch0 + a, j = batch / batches, part = batch - j * batches;
                     if (batch >= all) break;
-                    if (part == 0 && j >= job.stages_b && !suspended_wait(empty_b + sb, phase, &failed)) failed = 1;
+                    if (part == 0 && j >= job.stages_b) wait_or_fail(empty_b + sb, phase, &failed);
 #pragma unroll
                     for (uint32_t i = 0; i < 2; ++i) {
                         const uint32_t r = part * 64 + i * 32 + (me >> 3);
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
         for (uint32_t e = 0; e < 4 * kEach; ++e) place[e] = ((4 * half + e) ^ (r & 7)) << 4;
         uint32_t s = 0, phase = 0, sa = MT == 1 ? group : i, phase_a = 1;
         for (uint32_t k = 0; k < records; ++k) {
-            if (!suspended_wait(raw_full + s, phase, &failed)) failed = 1;
+            wait_or_fail(raw_full + s, phase, &failed);
             uint4 codes[kMine][kEach];
             uint2 scales = {};   // eight bytes
             const uint32_t rec = smem_u32(raw) + (s * MT + i) * kMicroRecordBytes;
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
                 if (q >= here) break;
                 if (mine) {
                     const uint32_t at = sa;
-                    if (!suspended_wait(empty_a + at, phase_a, &failed)) failed = 1;
+                    wait_or_fail(empty_a + at, phase_a, &failed);
                     const uint32_t dst = a_base + at * 16384, two = (q < 2 ? scales.x : scales.y) >> (16 * (q & 1));
 #pragma unroll
                     for (uint32_t h = 0; h < kEach; ++h) {
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
                 }
             }
         }
-        if (!suspended_wait(&done, 0, &failed)) failed = 1;
+        wait_or_fail(&done, 0, &failed);
         tcgen05_fence_after();
         // results: the warp's quarter of the lanes, every other 16 tokens of its tile
         const uint32_t quarter = warp & 3, row_in = quarter * 32 + lane, row = (row_tile + i) * kMicroRows + row_in;

@@ -9,7 +9,8 @@
 // pairs are few, a part of them. Sums go to the workspace. Launch 2 does the same over row tiles of down; it makes the hidden values
 // from launch 1's sums as it lays out a group's columns. The CTA that is the last one to finish a row tile adds the pairs of every
 // token, in the order of the token's choice and of the parts, so no sum depends on which CTA that was.
-// Both are bound by the chosen experts' bytes, which are read once for up to 16 pairs (see enec_micro_pieces.cuh for the products).
+// Both are bound by the chosen experts' bytes, which are read once for a group of an expert's pairs: as many as the digits of whole rows
+// leave room for, 16 up to 2304 columns, 8 at 4096, 4 at 7168, 1 at 14336 (see enec_micro_pieces.cuh for the products).
 #include "enec_micro_pieces.cuh"
 
 #include <cooperative_groups.h>

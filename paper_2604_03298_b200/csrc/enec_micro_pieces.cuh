@@ -11,12 +11,13 @@
 // instruction that is far from being the bound: a record of 128 x 256 weights arrives every 750 clocks at HBM's rate, and 16 tokens
 // (128 columns) take 260. The products of digits and weights are exact; the eight sums are added in fp32, the smallest first.
 //
-// What x loses: it is rounded to 2^-22 of the largest of its 32 neighbours (all bits of a bf16 value down to 2^-14 of the largest, of an
-// fp16 value down to 2^-11). A NaN or an infinity makes its column NaN.
+// What x loses: it is rounded to 2^-22 of the largest of its 32 neighbours, whatever weight that one meets (all bits of a bf16 value down to
+// 2^-14 of the largest, of an fp16 value down to 2^-11). A NaN or an infinity makes its column NaN.
 //
 // A CTA takes tasks: 128 rows (a row tile of a matrix) x a range of records of columns. One warp copies records in bulk into a ring, as
 // far ahead as the ring is long; one issues the matrix instructions, with two sets of sums in turn; sixteen make the digits and take
-// the results of one task while the next one's products run.
+// the results of one task while the next one's products run. Not so in lockstep, where the CTAs of a cluster join their sums behind every
+// task: there all warps meet, and no record of the next task is asked for before.
 #pragma once
 
 #include "enec_micro_mma.cuh"
@@ -277,9 +278,9 @@ __device__ __forceinline__ void piece_products(PieceShared& sh, uint8_t* smem, u
                 stage_digits(sh, warp - 2, threadIdx.x & 31, task, digits, values);
             }
             const uint32_t set = i & 1;
-            if (!warp_wait(sh.done + set, (i >> 1) & 1, &sh.failed)) sh.failed = 1;
+            wait_or_fail(sh.done + set, (i >> 1) & 1, &sh.failed);
             tcgen05_fence_after();
-            const bool ok = !warp_failed(&sh.failed);
+            const bool ok = !sh.failed;   // lane by lane: nothing but stores to global memory may depend on it
             take(i, tmem + set * (kPieceTokens * kPieces) + ((warp & 3) * 32 << 16), ok);
             tcgen05_fence_before();
             warp_arrive(sh.drained + set);

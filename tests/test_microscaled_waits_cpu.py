@@ -30,11 +30,13 @@ def test_the_wait_of_a_warp_has_one_answer():
     text = _source("enec_micro_mma.cuh")
     assert re.search(r"bool warp_wait\(.*?return __all_sync\(0xFFFFFFFFu, suspended_wait\(", text, re.S)
     assert re.search(r"bool warp_failed\(.*?return __any_sync\(0xFFFFFFFFu, \*flag\)", text, re.S)
-    assert text.count("suspended_wait(") == 1
+    # a wait lane by lane sets the flag and gives no answer
+    assert re.search(r"void wait_or_fail\([^{}]*{\s*if \(!mbar_try_wait\(bar, parity\) && !suspended_wait\(bar, parity, flag\)\) \*flag = 1;\s*}", text)
+    assert text.count("suspended_wait(") == 2
 
 
 def test_every_file_with_waits_is_looked_at():
-    with_waits = {f for f in os.listdir(CSRC) if f.startswith("enec_micro") and re.search(r"(suspended_wait|warp_wait|mbar_wait_bounded)\(", _source(f))}
+    with_waits = {f for f in os.listdir(CSRC) if f.startswith("enec_micro") and re.search(r"(suspended_wait|warp_wait|wait_or_fail|mbar_wait_bounded)\(", _source(f))}
     assert with_waits == {name for name, _, _ in ISSUING} | {"enec_micro_mma.cuh"}
 
 
@@ -42,9 +44,7 @@ def test_every_file_with_waits_is_looked_at():
 def test_only_issuing_warps_leave_lane_by_lane(name, begin, end):
     issuing, others = _parts(name, begin, end)
     assert "mma_" in issuing and "tcgen05_commit" in issuing and "suspended_wait(" in issuing
-    # a wait lane by lane sets the flag and nothing else
-    lane_by_lane = re.findall(r"if \([^;{}]*?!suspended_wait\([^;{}]*?\)\) (?:sh\.)?failed = 1;", others)
-    assert len(lane_by_lane) == others.count("suspended_wait(") and "warp_wait(" in others
+    assert "suspended_wait(" not in others and "warp_wait(" in others
     # in the issuing part instructions of the whole warp stand behind a __syncwarp() only, and the part ends with one
     assert issuing.rstrip().endswith("__syncwarp();")
     rest = re.sub(r"__syncwarp\(\);\s*if \(lockstep\) meet\(i\);", "", issuing)
@@ -57,7 +57,19 @@ def test_the_flag_divides_no_warp(name, begin, end):
     it for itself, stores depend on it and nothing else: those places are listed."""
     _, others = _parts(name, begin, end)
     alone = {"enec_micro_many.cu": ["if (failed) report(", "if (threadIdx.x < 512 && good && !failed && row < job.s.rows) {"],
-             "enec_micro_both.cu": ["if (failed && threadIdx.x == 0) report("], "enec_micro_pieces.cuh": []}[name]
+             "enec_micro_both.cu": ["if (failed && threadIdx.x == 0) report("], "enec_micro_pieces.cuh": ["const bool ok = !sh.failed;"]}[name]
     for line in others.split("\n"):
-        line = re.sub(r"(sh\.)?failed = [01];|&(sh\.)?failed|warp_failed|volatile int failed;", "", line)
+        line = re.sub(r"(sh\.)?failed = [01];|&(sh\.)?failed|warp_failed|volatile int failed;|wait_or_fail", "", line)
         assert not re.search(r"\bfailed\b", line) or any(a in line for a in alone), line
+
+
+@pytest.mark.parametrize("name", ["enec_micro_few.cu", "enec_micro_moe.cu"])
+def test_what_a_task_says_lane_by_lane_guards_stores_only(name):
+    """`ok` of a task's sums: in `take` a condition of a store; in `after` a way out, behind which stands no instruction of the whole warp."""
+    text = _source(name)
+    for found in re.finditer(r"\bok\b", text):
+        line = text[text.rindex("\n", 0, found.start()) + 1:text.index("\n", found.start())]
+        if "bool ok" in line or re.fullmatch(r"\s*(} else )?if \([^()]*(\([^()]*\))*[^()]*\bok && row < [\w.]+\)( {)?", line):
+            continue
+        assert line.strip() == "if (!last || !good || !ok) return;"
+        assert not re.search(WHOLE_WARP, text[found.end():text.index("false, [](uint32_t) {});", found.end())])
