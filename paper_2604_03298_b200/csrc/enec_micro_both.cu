@@ -4,10 +4,10 @@
 // products run. A CTA takes tile after tile. A stage is one record's 256 columns: a record lies in memory as the tensor cores want it in
 // shared memory, so a stage is a handful of bulk copies without a tensor map, and its scales go on to tensor memory as they are
 // (tcgen05.cp). At this rate a tile is bound by shared memory: a stage's 44 KB are written once, and its 4 matrix instructions read 10 KB
-// each, 85 KB in all or 664 clocks at 128 bytes a clock, for 392 clocks of instructions (98 each, measured); the kernel takes 840.
+// each, 85 KB in all or 664 clocks at 128 bytes a clock, for 392 clocks of instructions (98 each, measured); the kernel takes 870.
 // 256 x 192 would need 548 for the same work, but only three such stages fit, and no second set of sums: 2048 x 14336 x 4096 took
-// 85 us (1300 clocks a stage, and 9000 a tile for storing behind the products) against 68 us. Pairs of CTAs that share the tokens'
-// operand would read 57 KB.
+// 85 us (1300 clocks a stage, and 9000 a tile for storing behind the products) where this form took 68 (it takes that with
+// the streams in L2, 74 us cold). Pairs of CTAs that share the tokens' operand would read 57 KB.
 #include "enec_micro_mma.cuh"
 
 #include "enec_micro_launch.cuh"

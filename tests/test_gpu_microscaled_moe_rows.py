@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 
 # 13312 values are 52 records of columns, the last with four stages; 13568 has three, 14337 and 15000 two
-@pytest.mark.parametrize("tokens", [1, 4, 33])
+@pytest.mark.parametrize("tokens", [1, 33])
 @pytest.mark.parametrize("hidden, inter", [(200, 14336), (14336, 72), (13312, 40), (40, 13568), (14337, 33), (100, 15000)])
 def test_rows_beyond_four_stages(tokens, hidden, inter):
     check(tokens, hidden, inter, 3, 2, tokens % 2, seed=hidden + tokens)
