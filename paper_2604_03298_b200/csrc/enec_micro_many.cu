@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(ManyShape<MT, MAP>::kThreads, 1) enec_micro_ma
             if (half == 0 && group == 0) tops[i * 128 + r] = uint16_t((top - kFp16Up) << 1 | uint32_t(wide));
             asm volatile("bar.sync 1, %0;" ::"n"(Shape::kWeights) : "memory");
             factor = micro_scale(tops[i * 128 + row_in] >> 1);
-            wide_rows = __ballot_sync(0xFFFFFFFFu, row < job.s.rows && (tops[i * 128 + row_in] & 1));
+            wide_rows = __ballot_sync(0xFFFFFFFFu, good && row < job.s.rows && (tops[i * 128 + row_in] & 1));
             asm volatile("bar.sync 1, %0;" ::"n"(Shape::kWeights) : "memory");
         }
         if (!warp_failed(&failed) && steps > 0 && mine) {

@@ -58,8 +58,9 @@ __device__ __forceinline__ uint32_t mbar_complete(uint64_t* bar, uint32_t parity
 // instructions of the whole warp (votes, loads of tensor memory, barriers), and a warp in two parts would wait in them for good. So a
 // warp that leaves its loop then does so together (warp_wait), as it does by the flag by which a CTA gives up (warp_failed); the
 // warps that would feel the votes (2048 x 4096 x 4096: 58.2 instead of 56.1 us) set the flag and go on to the end of their loop, each
-// further wait one try long (wait_or_fail; with the first try outside the counted ones, which takes 1.7 us off). The warps that issue matrix instructions run no instruction of the whole warp but behind a
-// __syncwarp(), at the end of a task or of their part, and leave lane by lane.
+// further wait two tries long (wait_or_fail; its first try is not among the counted ones, which takes 1.7 us off; as long a try as
+// theirs or a mere question there cost 0.3 us). The warps that issue matrix instructions run no instruction of the whole warp but
+// behind a __syncwarp(), at the end of a task or of their part, and leave lane by lane.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
     return __all_sync(0xFFFFFFFFu, suspended_wait(bar, parity, abort_flag));
 }
